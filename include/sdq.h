@@ -96,7 +96,7 @@ enum {
 enum { SDQ_ORDER_LARGE = 0, SDQ_ORDER_SMALL = 1 };
 /* Inlier scale format (sdq_config.sfmt_i). */
 enum { SDQ_SCALE_DEFAULT = 0, SDQ_SCALE_E4M3 = 1, SDQ_SCALE_UE6M2 = 2 };
-enum { SDQ_DTYPE_F32 = 0, SDQ_DTYPE_BF16 = 1 };
+enum { SDQ_DTYPE_F32 = 0, SDQ_DTYPE_BF16 = 1, SDQ_DTYPE_E4M3 = 2 /* caches only */ };
 /* sdq_gemm_ex / sdq_gemm_ws kernel choice. */
 enum { SDQ_PATH_AUTO = 0, SDQ_PATH_DECODE = 1, SDQ_PATH_MFMA = 2, SDQ_PATH_DENSE = 3, SDQ_PATH_SPLITK = 4 };
 
@@ -449,6 +449,147 @@ sdq_status sdq_quantize_act_dual(const sdq_config* cfg, const void* X, int32_t x
 sdq_status sdq_gemm_dual(const sdq_config* cfg, const void* Xq_o, const float* s_a_o,
                          const void* Xq_i, const void* e_a_i, int64_t M, const void* packed,
                          int64_t N, int64_t K, void* Y, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The decode step between the projections: what a model that answers does
+ * with the output of its stacked q/k/v projection before the output
+ * projection reads it.  sdq_qkv_append normalizes and rotates queries and
+ * keys and writes the new keys and values into a paged cache;
+ * sdq_attn_decode attends over the cache with one new token per sequence;
+ * sdq_cache_evict keeps a long cache within a budget.
+ *
+ * A cache is `pages` pages of page_size slots for each of `heads` key heads.
+ * Sequence b's slot t lies on page page_table[b * table_stride + t /
+ * page_size] at offset t % page_size.  Page ids are the caller's to give out;
+ * entries past a sequence's end are not used.  An id outside [0, pages) counts
+ * as absent: nothing is read from or written to it, its slots are masked.
+ *
+ *   k, v      device, element (page, head, slot, d) at page * page_stride +
+ *             head * head_stride + slot * slot_stride + d, strides in
+ *             elements and shared by k and v.  Rows are 16-byte aligned: the
+ *             pointers, and the strides times the element size, are multiples
+ *             of 16 bytes.  Slots do not overlap.
+ *   dtype     SDQ_DTYPE_BF16, or SDQ_DTYPE_E4M3: e4m3 codes with one fp32
+ *             scale per row (k_scale, v_scale: device, [pages][heads]
+ *             [page_size]; NULL otherwise), by sdq_quantize_act's rule with
+ *             a row in the place of a token: s = amax / 448, code =
+ *             e4m3(x * (448 / amax)), a zero row s = 0 and zero codes.  A row
+ *             that holds an infinity or a NaN gets a scale that is not finite.
+ *   position  device, int32 [pages][heads][page_size]: the position of the
+ *             token in each slot, or NULL: not kept
+ *   weight    device, fp32 [pages][heads][page_size]: the attention weight
+ *             each slot has received, or NULL: not kept
+ *   heads     1 to 1024;  dim  a multiple of 16 up to 256;  page_size  1 to
+ *             2^20;  pages * page_size below 2^31
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t* position;
+  float* weight;
+  int64_t pages;
+  int64_t page_stride, head_stride, slot_stride;
+  int32_t dtype;
+  int32_t heads, page_size, dim;
+} sdq_kv_cache;
+
+/* What happens to queries and keys before attention.
+ *   heads_q      query heads, a multiple of the cache's heads, up to 1024
+ *   q_weight, k_weight  device, fp32 [dim], 16-byte aligned, both or neither:
+ *                every query (key) head becomes x * weight / sqrt(mean x^2 + eps)
+ *   cos_sin      device, fp32 [positions][rot_dim], 16-byte aligned: for each
+ *                position the rot_dim / 2 cosines, then the sines; NULL with
+ *                rot_dim = 0
+ *   rot_dim      leading dimensions of a head that are rotated: even, 0 to dim
+ *   interleaved  0: dimension i is paired with i + rot_dim / 2; 1: 2i with 2i + 1.
+ *                A pair (a, b) becomes (a cos - b sin, b cos + a sin). */
+typedef struct {
+  const float *q_weight, *k_weight;
+  const float* cos_sin;
+  int64_t positions;
+  int32_t heads_q, rot_dim, interleaved;
+  float eps;
+} sdq_qk_transform;
+
+/* Norm, rotation and append, in one pass over the projection's output.
+ *   qkv      device, M rows of heads_q queries, heads keys and heads values of
+ *            dim elements, row_stride elements apart, x_dtype SDQ_DTYPE_F32 or
+ *            SDQ_DTYPE_BF16, rows 16-byte aligned
+ *   pos      device, int32 [M]: positions, read where rot_dim > 0 or the
+ *            cache keeps positions (else may be NULL).  With rot_dim > 0, a token
+ *            whose position lies outside [0, positions) gets NaN queries and is
+ *            not appended.
+ *   slot     device, int64 [M]: page * page_size + offset of the token's slot;
+ *            outside [0, pages * page_size): not appended (a padding row).  Two
+ *            tokens of a call do not share a slot.
+ *   q_out    device, [M][heads_q][dim], q_dtype F32 or BF16 (nearest even),
+ *            16-byte aligned; does not overlap qkv
+ * Arithmetic is fp32; each result is rounded once.  A cache that keeps
+ * positions and weights gets pos[m] and 0 for the new slots.  M = 0 is a
+ * no-op; M * (heads_q + 2 heads) below 2^26. */
+sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_transform* t, const void* qkv,
+                          int32_t x_dtype, int64_t M, int64_t row_stride, const int32_t* pos,
+                          const int64_t* slot, void* q_out, int32_t q_dtype, void* stream);
+
+/* Attention of one new token per sequence over its first seq_lens[b] slots:
+ *   z_t = scale * q . k_t;  p = softmax(z);  out = sum_t p_t v_t
+ *   lse = log sum_t exp z_t
+ *   weight_out[slot t] = cache->weight[slot t] + sum over the query heads of
+ *                        the key head of p_t
+ *   q         device, [B][heads_q][dim], q_stride elements between sequences,
+ *             dtype SDQ_DTYPE_F32 or SDQ_DTYPE_BF16, 16-byte aligned rows.
+ *             Query head h reads key head h / (heads_q / heads).
+ *   page_table  device, int32, B rows of max_pages entries, table_stride apart
+ *   seq_lens  device, int32 [B]; clamped to [0, min(max_len, max_pages * page_size)]
+ *   max_len   an upper bound of the lengths that the host knows (it sizes the
+ *             launch, the workspace and nothing else)
+ *   out       device, [B][heads_q][dim] of the same dtype as q, 16-byte aligned
+ *   lse       device, fp32 [B][heads_q], or NULL
+ *   weight_out  device, as cache->weight, which it may be; or NULL.  Slots
+ *             past a sequence's end are not written.  Sequences share no page.
+ *   workspace device, 16-byte aligned, at least
+ *             sdq_attn_decode_workspace_size(cache, B, heads_q, max_len, track) bytes,
+ *             max_len as given here or min(max_len, max_pages * page_size), track:
+ *             weight_out is not NULL.  Scratch, as in sdq_gemm_ws.
+ * A sequence without a slot gives zeros and lse = -inf.  Scores, softmax and
+ * sums are fp32; the probabilities enter the second product with 17 bits (bf16
+ * outputs) or 24 (fp32).  Deterministic.  B = 0 is a no-op; B up to 2^20, with
+ * B * heads * ceil(heads_q / heads / 16) * ceil(max_len / 128) and the launches'
+ * other counts below 2^31. */
+sdq_status sdq_attn_decode_workspace_size(const sdq_kv_cache* cache, int64_t B, int32_t heads_q,
+                                          int64_t max_len, int32_t track, size_t* bytes);
+sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const void* q, int32_t dtype, int64_t B,
+                           int32_t heads_q, int64_t q_stride, const int32_t* page_table,
+                           int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
+                           int64_t max_len, float scale, void* out, float* lse, float* weight_out,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated attention weight, for caches that keep positions
+ * and weights.  In every sequence longer than `budget` slots, each key head
+ * keeps `budget` of them: first those whose position is above the head's
+ * newest minus `recent`, then those of the largest weight (a NaN counts as the
+ * lowest); equal weights go to the lowest slot, also among the recent ones
+ * where they alone exceed the budget.  Kept slots below the budget stay where
+ * they are; the i-th freed slot below it takes the i-th kept slot above it,
+ * with its key, value, scales, position and weight.  The order of slots is
+ * therefore no longer that of positions, which attention does not need.
+ *   page_table, seq_lens, max_len, table_stride, max_pages  as above
+ *   lens_out  device, int32 [B]: min(length, budget); may be seq_lens
+ *   position_out, weight_out  device, as cache->position and cache->weight:
+ *             either both those very pointers, or both apart from them.  Slots
+ *             below the new length get the kept slots' values, those from there
+ *             to the old length -1 and 0; others are not written.
+ *   workspace device, 16-byte aligned, sdq_cache_evict_workspace_size bytes
+ * Keys and values move in place; what lies in slots past the new length is not
+ * cleared, and pages wholly past it are the caller's again.  Sequences share
+ * no page.  1 <= budget, 0 <= recent <= budget.  B = 0 is a no-op. */
+sdq_status sdq_cache_evict_workspace_size(const sdq_kv_cache* cache, int64_t B, int64_t max_len,
+                                          int64_t budget, size_t* bytes);
+sdq_status sdq_cache_evict(const sdq_kv_cache* cache, int64_t B, const int32_t* page_table,
+                           int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
+                           int64_t max_len, int64_t budget, int64_t recent, int32_t* lens_out,
+                           int32_t* position_out, float* weight_out, void* workspace,
+                           size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -545,3 +545,11 @@ def gemm_path(cfg: Config, M: int, N: int, K: int, workspace: bool = False) -> i
     else:
         _lib.check(_lib.lib().sdq_gemm_path(cfg._ref, M, N, K, C.byref(p)), "sdq_gemm_path")
     return p.value
+
+
+# The paged key-value cache (kv.py uses the checks above).
+from .kv import (KVCache, attn_decode, attn_decode_workspace_size, cache_evict, cache_evict_workspace_size,  # noqa: E402
+                 qkv_append)
+
+__all__ += ["KVCache", "qkv_append", "attn_decode", "attn_decode_workspace_size", "cache_evict",
+            "cache_evict_workspace_size"]

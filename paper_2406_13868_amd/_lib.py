@@ -20,7 +20,7 @@ METRIC_MAGNITUDE, METRIC_PRODUCT = 0, 1
 DECOMP = {"same": 0, "magnitude": 1, "product": 2, "error": 3, "output_error": 4}
 ORDER = {"large": 0, "small": 1}
 SCALE = {"": 0, "e4m3": 1, "ue6m2": 2}
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 PATH_AUTO, PATH_DECODE, PATH_MFMA, PATH_DENSE, PATH_SPLITK = 0, 1, 2, 3, 4
 
 # Every exported symbol, as declared in include/sdq.h.
@@ -30,6 +30,8 @@ EXPORTS = (
     "sdq_gemm_path", "sdq_linear", "sdq_gemm_workspace_size", "sdq_gemm_ws",
     "sdq_quantize_act_dual", "sdq_gemm_dual", "sdq_gemm_static", "sdq_gemm_path_ws",
     "sdq_unpack_weights", "sdq_gemm_unpacked", "sdq_linear_ws",
+    "sdq_qkv_append", "sdq_attn_decode_workspace_size", "sdq_attn_decode",
+    "sdq_cache_evict_workspace_size", "sdq_cache_evict",
 )
 STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
@@ -40,6 +42,19 @@ class sdq_config(C.Structure):
                 ("fmt_i", C.c_int32), ("fmt_a", C.c_int32), ("metric", C.c_int32),
                 ("decomp", C.c_int32), ("order", C.c_int32), ("sfmt_i", C.c_int32),
                 ("y_dtype", C.c_int32), ("qv_i", C.c_int32)]
+
+
+class sdq_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("position", C.c_void_p), ("weight", C.c_void_p), ("pages", C.c_int64),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("dtype", C.c_int32), ("heads", C.c_int32), ("page_size", C.c_int32), ("dim", C.c_int32)]
+
+
+class sdq_qk_transform(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("cos_sin", C.c_void_p),
+                ("positions", C.c_int64), ("heads_q", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float)]
 
 
 class SDQError(RuntimeError):
@@ -119,6 +134,12 @@ def lib() -> C.CDLL:
             "sdq_gemm_static": (C.c_int, [cfgp, vp, vp, i64, vp, i64, i64, vp, vp, C.c_int32]),
             "sdq_unpack_weights": (C.c_int, [cfgp, vp, i64, i64, vp, C.c_size_t, vp]),
             "sdq_gemm_unpacked": (C.c_int, [cfgp, vp, vp, i64, vp, i64, i64, vp, C.c_size_t, vp, vp]),
+            "sdq_qkv_append": (C.c_int, [vp, vp, vp, C.c_int32, i64, i64, vp, vp, vp, C.c_int32, vp]),
+            "sdq_attn_decode_workspace_size": (C.c_int, [vp, i64, C.c_int32, i64, C.c_int32, P(C.c_size_t)]),
+            "sdq_attn_decode": (C.c_int, [vp, vp, C.c_int32, i64, C.c_int32, i64, vp, i64, i64, vp, i64, C.c_float,
+                                          vp, vp, vp, vp, C.c_size_t, vp]),
+            "sdq_cache_evict_workspace_size": (C.c_int, [vp, i64, i64, i64, P(C.c_size_t)]),
+            "sdq_cache_evict": (C.c_int, [vp, i64, vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, vp, C.c_size_t, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -39,6 +39,10 @@ SOURCES = [
     "gemm_mx_dense.hip",
     "gemm_dual.hip",
     "gemm_dual_decode.hip",
+    "abi_kv.hip",
+    "kv_append.hip",
+    "attn_decode.hip",
+    "cache_evict.hip",
 ]
 
 COMMON = [

@@ -1,0 +1,125 @@
+"""GPU: eviction against the oracle: which slots stay, where they move, and what is left alone."""
+import numpy as np
+import pytest
+
+from gpu_util import say, torch_cuda
+from kv_util import Pool
+from oracle import decode as O
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # lens, heads, D, page_size, kv, layout, budget, recent, weights
+    ([5], 1, 16, 1, "bf16", "hnd", 1, 0, "spread"),
+    ([5], 1, 16, 1, "bf16", "hnd", 1, 1, "spread"),
+    ([0, 1, 63, 64, 65, 200], 2, 64, 16, "bf16", "hnd", 64, 10, "spread"),
+    ([100, 2000, 1024, 1025], 3, 96, 24, "e4m3", "wide", 512, 0, "spread"),
+    ([100, 2000, 1024, 1025], 3, 96, 24, "e4m3", "nhd", 512, 512, "spread"),
+    ([3000, 2047], 2, 128, 64, "bf16", "nhd", 1500, 100, "equal"),
+    ([3000, 2047], 2, 80, 7, "e4m3", "hnd", 1500, 100, "few"),
+    ([2500, 40], 1, 256, 48, "bf16", "wide", 1100, 33, "odd"),
+    ([5000], 2, 32, 128, "bf16", "hnd", 4999, 5, "spread"),
+    ([5000], 2, 32, 128, "bf16", "hnd", 1, 0, "few"),
+]
+
+
+def _weights(rng, kind, shape):
+    if kind == "equal":
+        return np.full(shape, 0.25, np.float32)
+    if kind == "few":  # many ties, zeros of both signs among them
+        return rng.choice(np.array([0.0, -0.0, 0.5, 0.5, 2.0], np.float32), shape)
+    w = np.exp(3 * rng.standard_normal(shape)).astype(np.float32)
+    if kind == "odd":
+        w[rng.random(shape) < 0.2] = np.nan
+        w[rng.random(shape) < 0.2] = np.inf
+        w[rng.random(shape) < 0.2] = 1e-42
+        w[rng.random(shape) < 0.2] *= -1
+    return w
+
+
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) if not isinstance(x, list) else f"B{len(x)}x{max(x)}" for x in c))
+def test_eviction(case, apart):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+
+    lens, heads, D, ps, kvt, layout, budget, recent, kind = case
+    say("evict", case, apart)
+    rng = np.random.default_rng(budget + D)
+    pool = Pool(torch, sdq, rng, lens, heads, ps, D, kvt, layout, track=True, poison=False)
+    pool.weight = _weights(rng, kind, pool.weight.shape)
+    # distinct positions, in order for the first sequence and in none for the others
+    for b, n in enumerate(lens):
+        t = np.arange(n)
+        for h in range(heads):
+            pool.position[pool.table[b][t // ps], h, t % ps] = 3 * (t if b == 0 else rng.permutation(n))
+    cache = pool.cache
+    cache.weight.copy_(torch.from_numpy(pool.weight))
+    cache.position.copy_(torch.from_numpy(pool.position))
+    raw = lambda t: t.contiguous().view(torch.uint8 if pool.e4m3 else torch.int16).cpu().numpy().copy()  # noqa: E731
+    kv = [raw(cache.k), raw(cache.v)]
+    scales = [] if pool.ks is None else [pool.ks.numpy().copy(), pool.vs.numpy().copy()]
+    want_w, want_p = pool.weight.copy(), pool.position.copy()
+    if apart:
+        want_w, want_p = np.full_like(want_w, 7), np.full_like(want_p, 7)
+        w_out, p_out = torch.full_like(cache.weight, 7), torch.full_like(cache.position, 7)
+        lens_out = torch.full_like(pool.lens_gpu, -9)
+        got = sdq.cache_evict(cache, pool.table_gpu, pool.lens_gpu, budget, recent, weight_out=w_out, position_out=p_out, lens_out=lens_out)
+        assert got is lens_out
+        assert np.array_equal(cache.weight.cpu().numpy().view(np.int32), pool.weight.view(np.int32)) and np.array_equal(cache.position.cpu().numpy(), pool.position)
+    else:
+        w_out, p_out = cache.weight, cache.position
+        got = sdq.cache_evict(cache, pool.table_gpu, pool.lens_gpu, budget, recent, max_len=max(lens), lens_out=pool.lens_gpu)
+    torch.cuda.synchronize()
+    assert got.tolist() == [min(n, budget) for n in lens]
+    for b, n in enumerate(lens):
+        t = np.arange(n)
+        for h in range(heads):
+            at = lambda t: (pool.table[b][t // ps], h, t % ps)  # noqa: E731
+            of, to, w, p = O.evict(pool.weight[at(t)], pool.position[at(t)], budget, recent)
+            want_w[at(t)], want_p[at(t)] = w, p
+            for x in kv + scales:
+                x[at(to)] = x[at(of)]
+    assert np.array_equal(w_out.cpu().numpy().view(np.int32), want_w.view(np.int32))
+    assert np.array_equal(p_out.cpu().numpy(), want_p)
+    for got, want in zip((cache.k, cache.v), kv):
+        assert np.array_equal(raw(got), want)
+    for got, want in zip((cache.k_scale, cache.v_scale), scales):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_attention_does_not_depend_on_the_order_eviction_leaves():
+    """Attention over the evicted cache is attention over the kept slots."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+
+    rng = np.random.default_rng(11)
+    pool = Pool(torch, sdq, rng, [500, 90], 2, 16, 64, track=True)
+    t = np.arange(500)
+    kept = []
+    for h in range(2):
+        at = (pool.table[0][t // 16], h, t % 16)
+        pool.position[at] = t
+        _, _, _, p = O.evict(pool.weight[at], t.astype(np.int32), 200, 20)
+        kept.append(p[:200])
+    pool.cache.position.copy_(torch.from_numpy(pool.position))
+    q = rng.standard_normal((2, 4, 64)).astype(np.float32)
+    lens = sdq.cache_evict(pool.cache, pool.table_gpu, pool.lens_gpu, 200, 20)
+    out = sdq.attn_decode(torch.from_numpy(q).cuda(), pool.cache, pool.table_gpu, lens).cpu().numpy()
+    for h in range(2):
+        k, v = (pool.rows(O, x, 0, h)[kept[h]] for x in "kv")
+        want = O.attend(q[0, 2 * h:2 * h + 2], k, v, 64 ** -0.5)["out"]
+        assert np.allclose(out[0, 2 * h:2 * h + 2], want, rtol=1e-4, atol=1e-5)
+
+
+def test_absent_pages_and_no_sequences():
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+
+    rng = np.random.default_rng(2)
+    pool = Pool(torch, sdq, rng, [64], 1, 16, 32, track=True, poison=False)
+    before = pool.cache.k.clone()
+    table = torch.full_like(pool.table_gpu, -1)
+    assert sdq.cache_evict(pool.cache, table, pool.lens_gpu, 10).tolist() == [10]
+    assert torch.equal(pool.cache.k, before) and torch.equal(pool.cache.weight.cpu(), torch.from_numpy(pool.weight))
+    assert sdq.cache_evict(pool.cache, table[:0], pool.lens_gpu[:0], 10).shape == (0,)
