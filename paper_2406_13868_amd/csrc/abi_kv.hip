@@ -73,7 +73,7 @@ bool heads_fit(const sdq_kv_cache* c, int32_t heads_q) {
 // kernels' 32-bit indexes.
 bool attn_fits(const sdq_kv_cache* c, int64_t B, int32_t heads_q, int64_t cap) {
   const int64_t rows = int64_t(c->heads) * ((heads_q / c->heads + 15) / 16), lim = int64_t(1) << 31;
-  const int64_t chunks = (cap + 127) / 128 + 1, blocks = (cap + 255) / 256;
+  const int64_t chunks = (cap + 127) / 128 + 8, blocks = (cap + 255) / 256;
   return B * rows < lim / chunks && B * (heads_q + c->heads * blocks) < lim / 2;
 }
 

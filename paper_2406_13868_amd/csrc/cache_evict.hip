@@ -12,6 +12,8 @@
 // One workgroup selects for one key head of one sequence: a radix selection
 // over the weights' bits (three digits, counted in shared memory), then one
 // pass in slot order that settles ties and lists what moves by prefix sums.
+// Up to 32768 slots are read once and kept in registers (1 to 32 per thread,
+// the fewest that hold max_len); beyond, every pass reads them again from the L2.
 // A second kernel moves the rows, 16 bytes per lane.
 #include <hip/hip_runtime.h>
 
@@ -74,16 +76,53 @@ __device__ __forceinline__ int block_max(int v, int* waves) {
   return r;
 }
 
+// What selection needs of a slot.
+struct Slots {
+  const EvictArgs& a;
+  int b, n;
+  uint32_t h;
+  __device__ __forceinline__ int64_t at(int t) const { return Slot(a.kv, a.seqs, b, h, t).at; }
+  __device__ __forceinline__ int position(int t) const {
+    const int64_t i = t < n ? at(t) : -1;
+    return i >= 0 ? a.kv.position[i] : INT32_MIN;
+  }
+  __device__ __forceinline__ uint32_t key(int t) const {
+    const int64_t i = t < n ? at(t) : -1;
+    return i >= 0 ? order_bits(a.kv.weight[i]) : 0;
+  }
+};
+
+constexpr int kWaves = kSelect / 64;
+constexpr int kBatch = 32;  // steps of kSelect slots that are ranked together
+
+// Exclusive prefix sums of table[0 .. steps * kWaves) in place, plus `seen`,
+// which grows by their sum.
+__device__ __forceinline__ void scan_table(uint32_t* table, int steps, uint32_t* waves, uint32_t& seen) {
+  __syncthreads();
+  const int tid = threadIdx.x;
+  const uint32_t v = tid < steps * kWaves ? table[tid] : 0;
+  uint32_t all;
+  const uint32_t incl = block_scan(v, waves, all);
+  if (tid < steps * kWaves) table[tid] = seen + incl - v;
+  seen += all;
+  __syncthreads();
+}
+
 // lists: per row the number of moves, the new length, `most` destinations and
 // `most` sources.  The new lengths reach lens_out from the second kernel: it may
 // be seq_lens, which the workgroups of the other heads still read here.
-__global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a, int32_t* lists, int most) {
+// KEEP: slots per thread kept in registers; 0: read again in every pass.
+// Up to 8 the registers leave room for two workgroups on a compute unit.
+template <int KEEP>
+__global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, int32_t* lists, int most) {
   __shared__ uint32_t hist[kDigits];
-  __shared__ uint32_t waves[kSelect / 64];
+  __shared__ uint32_t table[kBatch * kWaves];
+  __shared__ uint32_t waves[kWaves];
   __shared__ uint32_t pick[2];
-  const int row = blockIdx.x, b = row / int(a.kv.heads), tid = threadIdx.x;
+  const int row = blockIdx.x, b = row / int(a.kv.heads), tid = threadIdx.x, wave = tid >> 6;
   const uint32_t h = row - b * int(a.kv.heads);
   const int n = seq_len(a.seqs, b), keep = min(n, a.budget);
+  const Slots slots{a, b, n, h};
   int32_t* list = lists + int64_t(row) * (2 + 2 * most);
   const bool in_place = a.weight_out == a.kv.weight;
   if (tid == 0) list[1] = keep;
@@ -91,28 +130,48 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a, int3
     if (tid == 0) list[0] = 0;
     if (!in_place)
       for (int t = tid; t < n; t += kSelect) {
-        const Slot s(a.kv, a.seqs, b, h, t);
-        if (s.at >= 0) {
-          a.weight_out[s.at] = a.kv.weight[s.at];
-          a.position_out[s.at] = a.kv.position[s.at];
+        const int64_t at = slots.at(t);
+        if (at >= 0) {
+          a.weight_out[at] = a.kv.weight[at];
+          a.position_out[at] = a.kv.position[at];
         }
       }
     return;
   }
 
+  const int steps = KEEP ? KEEP : (n + kSelect - 1) / kSelect;
+  constexpr int kRegs = KEEP ? KEEP : 1;
+  uint32_t key[kRegs];
+  uint32_t recent_bits = 0;  // of the thread's slots
   int newest = -1;
-  for (int t = tid; t < n; t += kSelect) {
-    const Slot s(a.kv, a.seqs, b, h, t);
-    if (s.at >= 0) newest = max(newest, a.kv.position[s.at]);
-  }
-  newest = block_max(newest, reinterpret_cast<int*>(waves));
-  // a slot is recent if position > newest - recent; 64 bits, since positions are the caller's
-  const int64_t edge = int64_t(newest) - a.recent;
+  // a slot is recent if position > edge; 64 bits, since positions are the caller's
+  int64_t edge;
   uint32_t recents = 0;
-  for (int t = tid; t < n; t += kSelect) {
-    const Slot s(a.kv, a.seqs, b, h, t);
-    if (s.at >= 0 && a.kv.position[s.at] > edge) ++recents;
+  if constexpr (KEEP > 0) {
+    int pos[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) {
+      pos[k] = slots.position(k * kSelect + tid);
+      key[k] = slots.key(k * kSelect + tid);
+    }
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) newest = max(newest, pos[k]);
+    newest = block_max(newest, reinterpret_cast<int*>(waves));
+    edge = int64_t(newest) - a.recent;
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) recent_bits |= uint32_t(k * kSelect + tid < n && pos[k] > edge) << k;
+    recents = __popc(recent_bits);
+  } else {
+    for (int k = 0; k < steps; ++k) newest = max(newest, slots.position(k * kSelect + tid));
+    newest = block_max(newest, reinterpret_cast<int*>(waves));
+    edge = int64_t(newest) - a.recent;
+    for (int k = 0; k < steps; ++k) recents += k * kSelect + tid < n && slots.position(k * kSelect + tid) > edge;
   }
+  const auto key_of = [&](int k) { return KEEP ? key[KEEP ? k : 0] : slots.key(k * kSelect + tid); };
+  const auto is_recent = [&](int k) {
+    if constexpr (KEEP > 0) return bool(recent_bits >> k & 1);
+    else return k * kSelect + tid < n && slots.position(k * kSelect + tid) > edge;
+  };
   uint32_t total;
   block_scan(recents, waves, total);
   // the class that is only partly kept, and how many of it
@@ -125,12 +184,11 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a, int3
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     for (int i = tid; i < kDigits; i += kSelect) hist[i] = 0;
     __syncthreads();
-    for (int t = tid; t < n; t += kSelect) {
-      const Slot s(a.kv, a.seqs, b, h, t);
-      const bool recent = s.at >= 0 && a.kv.position[s.at] > edge;
-      if (recent != among_recent) continue;
-      const uint32_t key = s.at >= 0 ? order_bits(a.kv.weight[s.at]) : 0;
-      if (pass == 0 || key >> (shift + bits) == prefix) atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1u);
+#pragma unroll kRegs
+    for (int k = 0; k < (KEEP ? KEEP : steps); ++k) {
+      if (k * kSelect + tid >= n || is_recent(k) != among_recent) continue;
+      const uint32_t x = key_of(k);
+      if (pass == 0 || x >> (shift + bits) == prefix) atomicAdd(&hist[x >> shift & ((1u << bits) - 1)], 1u);
     }
     __syncthreads();
     // digits from the largest down, two per thread
@@ -151,56 +209,81 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a, int3
 
   // in slot order: what stays, and what moves
   const bool ties = equal > want;
-  uint32_t eq_seen = 0, holes = 0, movers = 0;
-  for (int base = 0; base < n; base += kSelect) {
-    const int t = base + tid;
-    bool stays = false, is_eq = false;
-    int64_t at = -1;
-    if (t < n) {
-      const Slot s(a.kv, a.seqs, b, h, t);
-      at = s.at;
-      const bool recent = at >= 0 && a.kv.position[at] > edge;
-      if (recent == among_recent) {
-        const uint32_t key = at >= 0 ? order_bits(a.kv.weight[at]) : 0;
-        is_eq = key == prefix;
-        stays = key > prefix || is_eq;
-      } else {
-        stays = recent;
+  const uint64_t below = (uint64_t(1) << (tid & 63)) - 1;
+  uint32_t eq_seen = 0, moved = 0, n_holes = 0, n_movers = 0;
+  for (int base = 0; base < steps; base += kBatch) {
+    const int in_batch = min(kBatch, steps - base);
+    if (ties) {
+#pragma unroll kRegs
+      for (int j = 0; j < (KEEP ? KEEP : in_batch); ++j) {
+        const int k = KEEP ? j : base + j;
+        const bool eq = k * kSelect + tid < n && is_recent(k) == among_recent && key_of(k) == prefix;
+        const uint64_t m = __ballot(eq);
+        if ((tid & 63) == 0) table[j * kWaves + wave] = __popcll(m);
+      }
+      scan_table(table, in_batch, waves, eq_seen);
+    }
+    uint32_t stay_bits = 0;  // of this batch's slots
+#pragma unroll kRegs
+    for (int j = 0; j < (KEEP ? KEEP : in_batch); ++j) {
+      const int k = KEEP ? j : base + j, t = k * kSelect + tid;
+      const bool recent = is_recent(k), cls = t < n && recent == among_recent;
+      const uint32_t x = cls ? key_of(k) : 0;
+      const bool eq = cls && x == prefix;
+      bool stays = cls ? x > prefix || eq : t < n && recent;
+      if (ties) {
+        const uint64_t m = __ballot(eq);
+        if (eq) stays = table[j * kWaves + wave] + __popcll(m & below) < want;
+      }
+      stay_bits |= uint32_t(stays) << j;
+    }
+    __syncthreads();
+#pragma unroll kRegs
+    for (int j = 0; j < (KEEP ? KEEP : in_batch); ++j) {
+      const int t = (KEEP ? j : base + j) * kSelect + tid;
+      const bool stays = stay_bits >> j & 1;
+      const uint64_t holes = __ballot(t < keep && !stays), movers = __ballot(t >= keep && stays);
+      if ((tid & 63) == 0) table[j * kWaves + wave] = uint32_t(__popcll(holes)) | uint32_t(__popcll(movers)) << 16;
+    }
+    moved = 0;
+    scan_table(table, in_batch, waves, moved);
+#pragma unroll kRegs
+    for (int j = 0; j < (KEEP ? KEEP : in_batch); ++j) {
+      const int t = (KEEP ? j : base + j) * kSelect + tid;
+      const bool stays = stay_bits >> j & 1, hole = t < keep && !stays, mover = t >= keep && stays;
+      const uint64_t holes = __ballot(hole), movers = __ballot(mover);
+      const uint32_t first = table[j * kWaves + wave];
+      if (hole) list[2 + n_holes + (first & 0xFFFF) + __popcll(holes & below)] = t;
+      if (mover) list[2 + most + n_movers + (first >> 16) + __popcll(movers & below)] = t;
+    }
+    n_holes += moved & 0xFFFF;
+    n_movers += moved >> 16;
+    if (!in_place) {
+      for (int j = 0; j < in_batch; ++j) {
+        const int t = (base + j) * kSelect + tid;
+        const int64_t at = t < keep && (stay_bits >> j & 1) ? slots.at(t) : -1;
+        if (at >= 0) {
+          a.weight_out[at] = a.kv.weight[at];
+          a.position_out[at] = a.kv.position[at];
+        }
       }
     }
-    if (ties) {
-      uint32_t all;
-      const uint32_t rank = eq_seen + block_scan(is_eq, waves, all);
-      if (is_eq) stays = rank <= want;
-      eq_seen += all;
-    }
-    const bool hole = t < keep && !stays, mover = t >= keep && stays;
-    uint32_t all;
-    const uint32_t rank = block_scan(uint32_t(hole) | uint32_t(mover) << 16, waves, all);
-    if (hole) list[2 + holes + (rank & 0xFFFF) - 1] = t;
-    if (mover) list[2 + most + movers + (rank >> 16) - 1] = t;
-    holes += all & 0xFFFF;
-    movers += all >> 16;
-    if (!in_place && t < keep && stays && at >= 0) {
-      a.weight_out[at] = a.kv.weight[at];
-      a.position_out[at] = a.kv.position[at];
-    }
   }
-  if (tid == 0) list[0] = int32_t(holes);
+  if (tid == 0) list[0] = int32_t(n_holes);
   __syncthreads();
-  for (uint32_t i = tid; i < holes; i += kSelect) {
-    const Slot to(a.kv, a.seqs, b, h, list[2 + i]), of(a.kv, a.seqs, b, h, list[2 + most + i]);
-    if (to.at >= 0 && of.at >= 0) {
-      a.weight_out[to.at] = a.kv.weight[of.at];
-      a.position_out[to.at] = a.kv.position[of.at];
+  for (uint32_t i = tid; i < n_holes; i += kSelect) {
+    const int64_t to = slots.at(list[2 + i]), of = slots.at(list[2 + most + i]);
+    if (to >= 0 && of >= 0) {
+      a.weight_out[to] = a.kv.weight[of];
+      a.position_out[to] = a.kv.position[of];
     }
   }
   __syncthreads();
   for (int t = keep + tid; t < n; t += kSelect) {
-    const Slot s(a.kv, a.seqs, b, h, t);
-    if (s.at >= 0) {
-      a.weight_out[s.at] = 0.f;
-      a.position_out[s.at] = -1;
+    const int64_t at = slots.at(t);
+    if (at >= 0) {
+      a.weight_out[at] = 0.f;
+      a.position_out[at] = -1;
     }
   }
 }
@@ -251,7 +334,11 @@ size_t cache_evict_workspace_bytes(uint32_t heads_kv, int64_t B, int64_t cap, in
 
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const int most = int(most_moves(a.seqs.cap, a.budget)), rows = a.seqs.B * int(a.kv.heads);
-  evict_select_kernel<<<rows, kSelect, 0, st>>>(a, a.ws, most);
+  if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, a.ws, most);
+  else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, a.ws, most);
+  else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, a.ws, most);
+  else if (a.seqs.cap <= 32 * kSelect) evict_select_kernel<32><<<rows, kSelect, 0, st>>>(a, a.ws, most);
+  else evict_select_kernel<0><<<rows, kSelect, 0, st>>>(a, a.ws, most);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);

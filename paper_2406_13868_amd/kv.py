@@ -11,8 +11,27 @@ marshalled here and all work is done by the library's kernels.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 from . import _dev, _lib, _need, _need_bytes, _same_device, _stream, _torch, _workspace, _x_dtype
+
+# sdq_qk_transform as bytes: packing them takes a quarter of the time that
+# filling a ctypes structure does
+_TRANSFORM = struct.Struct("@PPPqiiif")
+assert _TRANSFORM.size == C.sizeof(_lib.sdq_qk_transform)
+
+
+def _ptr(t, shape, dtype, cache, what):
+    """The address of a contiguous tensor of this shape and type on the cache's
+    device: one cheap comparison each, and the named error where one fails."""
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == cache._index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(_need(t, shape, dtype, what), what)
+    _same_device(cache.k, t)
+    raise ValueError(f"{what} does not fit")
 
 
 class KVCache:
@@ -24,7 +43,7 @@ class KVCache:
     every slot.  The object holds the tensors; it owns no other memory."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "position", "weight", "pages", "heads", "page_size", "dim", "device",
-                 "_c", "_ref")
+                 "_c", "_ref", "_index")
 
     def __init__(self, k, v, k_scale=None, v_scale=None, position=None, weight=None):
         torch = _torch()
@@ -52,7 +71,7 @@ class KVCache:
         _same_device(k, v, k_scale, v_scale, position, weight)
         self.k, self.v, self.k_scale, self.v_scale, self.position, self.weight = k, v, k_scale, v_scale, position, weight
         self.pages, self.heads, self.page_size, self.dim = shape
-        self.device = k.device
+        self.device, self._index = k.device, k.get_device()
         for t, what in ((k, "k"), (v, "v")):
             if not t.is_cuda:
                 raise ValueError(f"{what} must be a CUDA (HIP) tensor")
@@ -90,18 +109,18 @@ def _no_overlap(shape, stride):
         at = s * n
 
 
-def _seqs(cache, page_table, seq_lens):
-    """B, and the page table's row stride."""
-    torch = _torch()
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.dtype != torch.int32:
+def _seqs(cache, page_table, seq_lens, torch):
+    """Of the page table: B, its width, its row stride and its address; the address of seq_lens."""
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.dtype is not torch.int32:
         raise ValueError("page_table must be [sequences, pages] int32")
     B, width = page_table.shape
-    _need(seq_lens, (B,), torch.int32, "seq_lens")
-    if width > 1 and page_table.stride(1) != 1:
+    lens = _ptr(seq_lens, (B,), torch.int32, cache, "seq_lens")
+    ld, step = page_table.stride()
+    if step != 1 and width > 1:
         raise ValueError("the rows of page_table must be contiguous")
-    if not page_table.is_cuda:
-        raise ValueError("page_table must be a CUDA (HIP) tensor")
-    return B, width, page_table.stride(0) if B > 1 else width
+    if page_table.get_device() != cache._index:
+        _same_device(cache.k, page_table)
+    return B, width, ld if B > 1 else width, page_table.data_ptr(), lens
 
 
 def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, interleaved: bool = False, q_weight=None,
@@ -121,36 +140,37 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     dim = cache.dim
     if heads_q < 1 or width != (heads_q + 2 * cache.heads) * dim:
         raise ValueError(f"qkv must be [M, {(heads_q + 2 * cache.heads) * dim}], got {list(qkv.shape)}")
-    if qkv.stride(1) != 1 or not qkv.is_cuda:
+    ld, step = qkv.stride()
+    if step != 1 or not qkv.is_cuda:
         raise ValueError("qkv must be a CUDA (HIP) tensor with contiguous rows")
+    if qkv.get_device() != cache._index:
+        _same_device(cache.k, qkv)
     dt = _x_dtype(qkv)
-    _need(slot, (M,), torch.int64, "slot")
+    at = _ptr(slot, (M,), torch.int64, cache, "slot")
+    where = qw = kw = angles = None
+    rot = positions = 0
     if pos is not None:
-        _need(pos, (M,), torch.int32, "pos")
+        where = _ptr(pos, (M,), torch.int32, cache, "pos")
     elif cos_sin is not None or cache.position is not None:
         raise ValueError("pos is needed for the rotation and for a cache that keeps positions")
-    rot, positions = 0, 0
     if cos_sin is not None:
-        if cos_sin.dim() != 2 or cos_sin.dtype != torch.float32:
+        if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2:
             raise ValueError("cos_sin must be [positions, rot_dim] float32")
         positions, rot = cos_sin.shape
-    if (q_weight is None) != (k_weight is None):
+        angles = _ptr(cos_sin, (positions, rot), torch.float32, cache, "cos_sin")
+    if q_weight is not None and k_weight is not None:
+        qw = _ptr(q_weight, (dim,), torch.float32, cache, "q_weight")
+        kw = _ptr(k_weight, (dim,), torch.float32, cache, "k_weight")
+    elif q_weight is not None or k_weight is not None:
         raise ValueError("q_weight and k_weight go together")
-    if q_weight is not None:
-        _need(q_weight, (dim,), torch.float32, "q_weight")
-        _need(k_weight, (dim,), torch.float32, "k_weight")
     if out is None:
         out = torch.empty((M, heads_q, dim), dtype=out_dtype or qkv.dtype, device=qkv.device)
-    else:
-        _need(out, (M, heads_q, dim), out_dtype or out.dtype, "out")
-    _same_device(qkv, pos, slot, cache.k, cos_sin, q_weight, k_weight, out)
-    t = _lib.sdq_qk_transform(None if q_weight is None else _dev(q_weight, "q_weight"),
-                              None if k_weight is None else _dev(k_weight, "k_weight"),
-                              _dev(cos_sin, "cos_sin") if rot else None, positions, heads_q, rot, interleaved, eps)
-    _lib.check(_lib.lib().sdq_qkv_append(cache._ref, C.byref(t), qkv.data_ptr(), dt, M,
-                                         qkv.stride(0) if M > 1 else width, None if pos is None else _dev(pos, "pos"),
-                                         _dev(slot, "slot"), _dev(out, "out"), _x_dtype(out), _stream(stream)),
-               "sdq_qkv_append")
+    to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
+    t = _TRANSFORM.pack(qw or 0, kw or 0, angles if rot else 0, positions, heads_q, rot, interleaved, eps)
+    rc = _lib.lib().sdq_qkv_append(cache._ref, t, qkv.data_ptr(), dt, M, ld if M > 1 else width, where, at, to, _x_dtype(out),
+                                   _stream(stream))
+    if rc:
+        _lib.check(rc, "sdq_qkv_append")
     return out
 
 
@@ -175,39 +195,40 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     head.  workspace: a uint8 tensor of attn_decode_workspace_size bytes, or a
     fresh one is made."""
     torch = _torch()
-    B, width, ld = _seqs(cache, page_table, seq_lens)
-    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != B or q.shape[2] != cache.dim:
-        raise ValueError(f"q must be [{B}, heads_q, {cache.dim}]")
+    B, width, ld, table, lens = _seqs(cache, page_table, seq_lens, torch)
+    dim = cache.dim
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != B or q.shape[2] != dim:
+        raise ValueError(f"q must be [{B}, heads_q, {dim}]")
     heads_q = q.shape[1]
     dt = _x_dtype(q)
-    if not q.is_cuda or q.stride(2) != 1 or (heads_q > 1 and q.stride(1) != cache.dim):
+    q_ld, head_ld, step = q.stride()
+    if not q.is_cuda or step != 1 or (heads_q > 1 and head_ld != dim):
         raise ValueError("q must be a CUDA (HIP) tensor whose sequences are contiguous")
+    if q.get_device() != cache._index:
+        _same_device(cache.k, q)
     if out is None:
-        out = torch.empty((B, heads_q, cache.dim), dtype=q.dtype, device=q.device)
-    else:
-        _need(out, q.shape, q.dtype, "out")
-    if lse is not None:
-        _need(lse, (B, heads_q), torch.float32, "lse")
+        out = torch.empty((B, heads_q, dim), dtype=q.dtype, device=q.device)
+    to = _ptr(out, (B, heads_q, dim), q.dtype, cache, "out")
+    log = None if lse is None else _ptr(lse, (B, heads_q), torch.float32, cache, "lse")
+    weights = None
     if weight_out is not None:
         if cache.weight is None:
             raise ValueError("weight_out needs a cache that keeps weights")
-        _need(weight_out, cache.weight.shape, torch.float32, "weight_out")
+        weights = _ptr(weight_out, cache.weight.shape, torch.float32, cache, "weight_out")
     cap = width * cache.page_size
     if max_len is not None and max_len < cap:
         cap = max_len
-    _same_device(q, cache.k, page_table, seq_lens, out, lse, weight_out, workspace)
-    track = weight_out is not None
     if workspace is None:
-        need = attn_decode_workspace_size(cache, B, heads_q, cap, track)
-        workspace = _workspace(need, q.device, stream)
+        workspace = _workspace(attn_decode_workspace_size(cache, B, heads_q, cap, weights is not None), q.device, stream)
+    elif workspace.get_device() != cache._index:
+        _same_device(cache.k, workspace)
     rc = _lib.lib().sdq_attn_decode(
-        cache._ref, q.data_ptr(), dt, B, heads_q, q.stride(0) if B > 1 else heads_q * cache.dim, page_table.data_ptr(),
-        ld, width, _dev(seq_lens, "seq_lens"), cap, cache.dim ** -0.5 if scale is None else scale, _dev(out, "out"),
-        None if lse is None else _dev(lse, "lse"), _dev(weight_out, "weight_out") if track else None,
-        _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
-    if rc == _lib.ERR_BUFFER_TOO_SMALL:
-        _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, track), "workspace")
-    _lib.check(rc, "sdq_attn_decode")
+        cache._ref, q.data_ptr(), dt, B, heads_q, q_ld if B > 1 else heads_q * dim, table, ld, width, lens, cap,
+        dim ** -0.5 if scale is None else scale, to, log, weights, _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
+    if rc:
+        if rc == _lib.ERR_BUFFER_TOO_SMALL:
+            _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights is not None), "workspace")
+        _lib.check(rc, "sdq_attn_decode")
     return out
 
 
@@ -229,31 +250,30 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
     place too, or written to position_out and weight_out (both, and not the
     cache's own)."""
     torch = _torch()
-    B, width, ld = _seqs(cache, page_table, seq_lens)
+    B, width, ld, table, lens = _seqs(cache, page_table, seq_lens, torch)
     if cache.position is None or cache.weight is None:
         raise ValueError("eviction needs a cache that keeps positions and weights")
     if (weight_out is None) != (position_out is None):
         raise ValueError("weight_out and position_out go together")
     if weight_out is None:
         weight_out, position_out = cache.weight, cache.position
-    _need(weight_out, cache.weight.shape, torch.float32, "weight_out")
-    _need(position_out, cache.weight.shape, torch.int32, "position_out")
+    shape = cache.weight.shape
+    weights = _ptr(weight_out, shape, torch.float32, cache, "weight_out")
+    positions = _ptr(position_out, shape, torch.int32, cache, "position_out")
     if lens_out is None:
         lens_out = torch.empty_like(seq_lens)
-    else:
-        _need(lens_out, (B,), torch.int32, "lens_out")
+    new = _ptr(lens_out, (B,), torch.int32, cache, "lens_out")
     cap = width * cache.page_size
     if max_len is not None and max_len < cap:
         cap = max_len
-    _same_device(cache.k, page_table, seq_lens, lens_out, weight_out, position_out, workspace)
     if workspace is None:
-        need = cache_evict_workspace_size(cache, B, cap, budget)
-        workspace = _workspace(need, cache.device, stream)
-    rc = _lib.lib().sdq_cache_evict(
-        cache._ref, B, page_table.data_ptr(), ld, width, _dev(seq_lens, "seq_lens"), cap, budget, recent,
-        _dev(lens_out, "lens_out"), _dev(position_out, "position_out"), _dev(weight_out, "weight_out"),
-        _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
-    if rc == _lib.ERR_BUFFER_TOO_SMALL:
-        _need_bytes(workspace, cache_evict_workspace_size(cache, B, cap, budget), "workspace")
-    _lib.check(rc, "sdq_cache_evict")
+        workspace = _workspace(cache_evict_workspace_size(cache, B, cap, budget), cache.device, stream)
+    elif workspace.get_device() != cache._index:
+        _same_device(cache.k, workspace)
+    rc = _lib.lib().sdq_cache_evict(cache._ref, B, table, ld, width, lens, cap, budget, recent, new, positions, weights,
+                                    _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
+    if rc:
+        if rc == _lib.ERR_BUFFER_TOO_SMALL:
+            _need_bytes(workspace, cache_evict_workspace_size(cache, B, cap, budget), "workspace")
+        _lib.check(rc, "sdq_cache_evict")
     return lens_out

@@ -132,6 +132,7 @@ class _Stub:
     pages, heads, page_size, dim, device = 4, 2, 8, 32, torch.device("cpu")
     k = v = torch.zeros((4, 2, 8, 32), dtype=torch.bfloat16)
     k_scale = v_scale = position = weight = None
+    _index = -1
 
 
 def test_the_binding_checks_the_calls():
