@@ -493,28 +493,11 @@ typedef struct {
   int32_t heads, page_size, dim;
 } sdq_kv_cache;
 
-/* What happens to queries and keys before attention.
- *   heads_q      query heads, a multiple of the cache's heads, up to 1024
- *   q_weight, k_weight  device, fp32 [dim], 16-byte aligned, both or neither:
- *                every query (key) head becomes x * weight / sqrt(mean x^2 + eps)
- *   cos_sin      device, fp32 [positions][rot_dim], 16-byte aligned: for each
- *                position the rot_dim / 2 cosines, then the sines; NULL with
- *                rot_dim = 0
- *   rot_dim      leading dimensions of a head that are rotated: even, 0 to dim
- *   interleaved  0: dimension i is paired with i + rot_dim / 2; 1: 2i with 2i + 1.
- *                A pair (a, b) becomes (a cos - b sin, b cos + a sin). */
-typedef struct {
-  const float *q_weight, *k_weight;
-  const float* cos_sin;
-  int64_t positions;
-  int32_t heads_q, rot_dim, interleaved;
-  float eps;
-} sdq_qk_transform;
-
 /* Norm, rotation and append, in one pass over the projection's output.
  *   qkv      device, M rows of heads_q queries, heads keys and heads values of
  *            dim elements, row_stride elements apart, x_dtype SDQ_DTYPE_F32 or
- *            SDQ_DTYPE_BF16, rows 16-byte aligned
+ *            SDQ_DTYPE_BF16, rows 16-byte aligned.  heads_q is a multiple of the
+ *            cache's heads, up to 1024.
  *   pos      device, int32 [M]: positions, read where rot_dim > 0 or the
  *            cache keeps positions (else may be NULL).  With rot_dim > 0, a token
  *            whose position lies outside [0, positions) gets NaN queries and is
@@ -524,12 +507,28 @@ typedef struct {
  *            tokens of a call do not share a slot.
  *   q_out    device, [M][heads_q][dim], q_dtype F32 or BF16 (nearest even),
  *            16-byte aligned; does not overlap qkv
+ *   q_weight, k_weight  device, fp32 [dim], 16-byte aligned, both or neither:
+ *            every query (key) head becomes x * weight / sqrt(mean x^2 + eps)
+ *   cos_sin  device, fp32 [positions][rot_dim], 16-byte aligned: for each
+ *            position the rot_dim / 2 cosines, then the sines; NULL with
+ *            rot_dim = 0
+ *   rot_dim  leading dimensions of a head that are rotated: even, 0 to dim
+ *   interleaved  0: dimension i is paired with i + rot_dim / 2; 1: 2i with 2i + 1.
+ *            A pair (a, b) becomes (a cos - b sin, b cos + a sin).
  * Arithmetic is fp32; each result is rounded once.  A cache that keeps
  * positions and weights gets pos[m] and 0 for the new slots.  M = 0 is a
  * no-op; M * (heads_q + 2 heads) below 2^26. */
-sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_transform* t, const void* qkv,
-                          int32_t x_dtype, int64_t M, int64_t row_stride, const int32_t* pos,
-                          const int64_t* slot, void* q_out, int32_t q_dtype, void* stream);
+typedef struct {
+  const void* qkv;
+  const int32_t* pos;
+  const int64_t* slot;
+  void* q_out;
+  const float *q_weight, *k_weight, *cos_sin;
+  int64_t M, row_stride, positions;
+  int32_t x_dtype, q_dtype, heads_q, rot_dim, interleaved;
+  float eps;
+} sdq_append_args;
+sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_append_args* args, void* stream);
 
 /* Attention of one new token per sequence over its first seq_lens[b] slots:
  *   z_t = scale * q . k_t;  p = softmax(z);  out = sum_t p_t v_t
@@ -542,7 +541,7 @@ sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_transform* t, 
  *   page_table  device, int32, B rows of max_pages entries, table_stride apart
  *   seq_lens  device, int32 [B]; clamped to [0, min(max_len, max_pages * page_size)]
  *   max_len   an upper bound of the lengths that the host knows (it sizes the
- *             launch, the workspace and nothing else)
+ *             launch and the workspace, and cuts what is longer)
  *   out       device, [B][heads_q][dim] of the same dtype as q, 16-byte aligned
  *   lse       device, fp32 [B][heads_q], or NULL
  *   weight_out  device, as cache->weight, which it may be; or NULL.  Slots
@@ -556,13 +555,20 @@ sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_transform* t, 
  * outputs) or 24 (fp32).  Deterministic.  B = 0 is a no-op; B up to 2^20, with
  * B * heads * ceil(heads_q / heads / 16) * ceil(max_len / 128) and the launches'
  * other counts below 2^31. */
+typedef struct {
+  const void* q;
+  const int32_t *page_table, *seq_lens;
+  void* out;
+  float *lse, *weight_out;
+  void* workspace;
+  size_t ws_bytes;
+  int64_t B, q_stride, table_stride, max_pages, max_len;
+  int32_t dtype, heads_q;
+  float scale;
+} sdq_attn_args;
 sdq_status sdq_attn_decode_workspace_size(const sdq_kv_cache* cache, int64_t B, int32_t heads_q,
                                           int64_t max_len, int32_t track, size_t* bytes);
-sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const void* q, int32_t dtype, int64_t B,
-                           int32_t heads_q, int64_t q_stride, const int32_t* page_table,
-                           int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
-                           int64_t max_len, float scale, void* out, float* lse, float* weight_out,
-                           void* workspace, size_t ws_bytes, void* stream);
+sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_args* args, void* stream);
 
 /* Eviction by accumulated attention weight, for caches that keep positions
  * and weights.  In every sequence longer than `budget` slots, each key head
@@ -573,7 +579,7 @@ sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const void* q, int32_t dty
  * they are; the i-th freed slot below it takes the i-th kept slot above it,
  * with its key, value, scales, position and weight.  The order of slots is
  * therefore no longer that of positions, which attention does not need.
- *   page_table, seq_lens, max_len, table_stride, max_pages  as above
+ *   page_table, seq_lens, B, table_stride, max_pages, max_len  as above
  *   lens_out  device, int32 [B]: min(length, budget); may be seq_lens
  *   position_out, weight_out  device, as cache->position and cache->weight:
  *             either both those very pointers, or both apart from them.  Slots
@@ -583,13 +589,17 @@ sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const void* q, int32_t dty
  * Keys and values move in place; what lies in slots past the new length is not
  * cleared, and pages wholly past it are the caller's again.  Sequences share
  * no page.  1 <= budget, 0 <= recent <= budget.  B = 0 is a no-op. */
+typedef struct {
+  const int32_t *page_table, *seq_lens;
+  int32_t *lens_out, *position_out;
+  float* weight_out;
+  void* workspace;
+  size_t ws_bytes;
+  int64_t B, table_stride, max_pages, max_len, budget, recent;
+} sdq_evict_args;
 sdq_status sdq_cache_evict_workspace_size(const sdq_kv_cache* cache, int64_t B, int64_t max_len,
                                           int64_t budget, size_t* bytes);
-sdq_status sdq_cache_evict(const sdq_kv_cache* cache, int64_t B, const int32_t* page_table,
-                           int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
-                           int64_t max_len, int64_t budget, int64_t recent, int32_t* lens_out,
-                           int32_t* position_out, float* weight_out, void* workspace,
-                           size_t ws_bytes, void* stream);
+sdq_status sdq_cache_evict(const sdq_kv_cache* cache, const sdq_evict_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -51,10 +51,24 @@ class sdq_kv_cache(C.Structure):
                 ("dtype", C.c_int32), ("heads", C.c_int32), ("page_size", C.c_int32), ("dim", C.c_int32)]
 
 
-class sdq_qk_transform(C.Structure):
-    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("cos_sin", C.c_void_p),
-                ("positions", C.c_int64), ("heads_q", C.c_int32), ("rot_dim", C.c_int32),
-                ("interleaved", C.c_int32), ("eps", C.c_float)]
+_PTR, _I64, _I32 = C.c_void_p, C.c_int64, C.c_int32
+
+
+class sdq_append_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("qkv", "pos", "slot", "q_out", "q_weight", "k_weight", "cos_sin")] + [
+        (n, _I64) for n in ("M", "row_stride", "positions")] + [
+        (n, _I32) for n in ("x_dtype", "q_dtype", "heads_q", "rot_dim", "interleaved")] + [("eps", C.c_float)]
+
+
+class sdq_attn_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("q", "page_table", "seq_lens", "out", "lse", "weight_out", "workspace")] + [
+        ("ws_bytes", C.c_size_t)] + [(n, _I64) for n in ("B", "q_stride", "table_stride", "max_pages", "max_len")] + [
+        ("dtype", _I32), ("heads_q", _I32), ("scale", C.c_float)]
+
+
+class sdq_evict_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("page_table", "seq_lens", "lens_out", "position_out", "weight_out", "workspace")] + [
+        ("ws_bytes", C.c_size_t)] + [(n, _I64) for n in ("B", "table_stride", "max_pages", "max_len", "budget", "recent")]
 
 
 class SDQError(RuntimeError):
@@ -134,12 +148,11 @@ def lib() -> C.CDLL:
             "sdq_gemm_static": (C.c_int, [cfgp, vp, vp, i64, vp, i64, i64, vp, vp, C.c_int32]),
             "sdq_unpack_weights": (C.c_int, [cfgp, vp, i64, i64, vp, C.c_size_t, vp]),
             "sdq_gemm_unpacked": (C.c_int, [cfgp, vp, vp, i64, vp, i64, i64, vp, C.c_size_t, vp, vp]),
-            "sdq_qkv_append": (C.c_int, [vp, vp, vp, C.c_int32, i64, i64, vp, vp, vp, C.c_int32, vp]),
+            "sdq_qkv_append": (C.c_int, [vp, vp, vp]),
             "sdq_attn_decode_workspace_size": (C.c_int, [vp, i64, C.c_int32, i64, C.c_int32, P(C.c_size_t)]),
-            "sdq_attn_decode": (C.c_int, [vp, vp, C.c_int32, i64, C.c_int32, i64, vp, i64, i64, vp, i64, C.c_float,
-                                          vp, vp, vp, vp, C.c_size_t, vp]),
+            "sdq_attn_decode": (C.c_int, [vp, vp, vp]),
             "sdq_cache_evict_workspace_size": (C.c_int, [vp, i64, i64, i64, P(C.c_size_t)]),
-            "sdq_cache_evict": (C.c_int, [vp, i64, vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, vp, C.c_size_t, vp]),
+            "sdq_cache_evict": (C.c_int, [vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

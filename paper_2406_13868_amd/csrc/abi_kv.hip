@@ -83,37 +83,38 @@ void drop_pending_error() { (void)hipGetLastError(); }
 
 }  // namespace
 
-extern "C" sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_transform* t, const void* qkv,
-                                     int32_t x_dtype, int64_t M, int64_t row_stride, const int32_t* pos,
-                                     const int64_t* slot, void* q_out, int32_t q_dtype, void* stream) {
+extern "C" sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_append_args* t, void* stream) {
   AppendArgs a;
   const sdq_status s = check_cache(cache, &a.kv);
   if (s != SDQ_OK) return s;
   if (!t) return SDQ_ERR_NULL;
-  if ((x_dtype != SDQ_DTYPE_F32 && x_dtype != SDQ_DTYPE_BF16) || (q_dtype != SDQ_DTYPE_F32 && q_dtype != SDQ_DTYPE_BF16))
+  if ((t->x_dtype != SDQ_DTYPE_F32 && t->x_dtype != SDQ_DTYPE_BF16) ||
+      (t->q_dtype != SDQ_DTYPE_F32 && t->q_dtype != SDQ_DTYPE_BF16))
     return SDQ_ERR_CONFIG;
   if (t->rot_dim < 0 || t->rot_dim > cache->dim || t->rot_dim % 2 || (t->interleaved != 0 && t->interleaved != 1) ||
       !t->q_weight != !t->k_weight || (t->q_weight && !(t->eps >= 0.f && std::isfinite(t->eps))))
     return SDQ_ERR_CONFIG;
-  const int64_t heads = int64_t(t->heads_q) + 2 * cache->heads;
+  const int64_t heads = int64_t(t->heads_q) + 2 * cache->heads, M = t->M;
   if (!heads_fit(cache, t->heads_q) || M < 0 || M > ((int64_t(1) << 26) - 1) / heads || t->positions < 0 ||
       t->positions >= (int64_t(1) << 31))
     return SDQ_ERR_SHAPE;
-  const int64_t elt = x_dtype == SDQ_DTYPE_F32 ? 4 : 2;
-  if (row_stride < heads * cache->dim || row_stride > (int64_t(1) << 40) || row_stride * elt % 16) return SDQ_ERR_SHAPE;
-  if (M == 0) return SDQ_OK;
-  if (!qkv || !slot || !q_out || (t->rot_dim && !t->cos_sin) || ((t->rot_dim || cache->position) && !pos))
-    return SDQ_ERR_NULL;
-  if (!aligned16(qkv) || !aligned16(q_out) || !aligned16(t->q_weight) || !aligned16(t->k_weight) || !aligned16(t->cos_sin))
+  const int64_t elt = t->x_dtype == SDQ_DTYPE_F32 ? 4 : 2;
+  if (t->row_stride < heads * cache->dim || t->row_stride > (int64_t(1) << 40) || t->row_stride * elt % 16)
     return SDQ_ERR_SHAPE;
-  a.qkv = qkv;
-  a.row_stride = row_stride;
-  a.pos = pos;
-  a.slot = slot;
+  if (M == 0) return SDQ_OK;
+  if (!t->qkv || !t->slot || !t->q_out || (t->rot_dim && !t->cos_sin) || ((t->rot_dim || cache->position) && !t->pos))
+    return SDQ_ERR_NULL;
+  if (!aligned16(t->qkv) || !aligned16(t->q_out) || !aligned16(t->q_weight) || !aligned16(t->k_weight) ||
+      !aligned16(t->cos_sin))
+    return SDQ_ERR_SHAPE;
+  a.qkv = t->qkv;
+  a.row_stride = t->row_stride;
+  a.pos = t->pos;
+  a.slot = t->slot;
   a.q_weight = t->q_weight;
   a.k_weight = t->k_weight;
   a.cos_sin = t->cos_sin;
-  a.q_out = q_out;
+  a.q_out = t->q_out;
   a.positions = t->positions;
   a.M = uint32_t(M);
   a.heads_q = uint32_t(t->heads_q);
@@ -122,7 +123,7 @@ extern "C" sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_qk_tra
   a.interleaved = t->interleaved != 0;
   drop_pending_error();
   const hipError_t e =
-      launch_qkv_append(a, x_dtype == SDQ_DTYPE_F32, q_dtype == SDQ_DTYPE_F32, static_cast<hipStream_t>(stream));
+      launch_qkv_append(a, t->x_dtype == SDQ_DTYPE_F32, t->q_dtype == SDQ_DTYPE_F32, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SDQ_OK : SDQ_ERR_HIP;
 }
 
@@ -138,40 +139,38 @@ extern "C" sdq_status sdq_attn_decode_workspace_size(const sdq_kv_cache* cache, 
   return SDQ_OK;
 }
 
-extern "C" sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const void* q, int32_t dtype, int64_t B,
-                                      int32_t heads_q, int64_t q_stride, const int32_t* page_table,
-                                      int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
-                                      int64_t max_len, float scale, void* out, float* lse, float* weight_out,
-                                      void* workspace, size_t ws_bytes, void* stream) {
+extern "C" sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_args* t, void* stream) {
   AttnArgs a;
   sdq_status s = check_cache(cache, &a.kv);
   if (s != SDQ_OK) return s;
-  if (dtype != SDQ_DTYPE_F32 && dtype != SDQ_DTYPE_BF16) return SDQ_ERR_CONFIG;
-  s = check_seqs(cache, B, page_table, table_stride, max_pages, seq_lens, max_len, &a.seqs);
+  if (!t) return SDQ_ERR_NULL;
+  if (t->dtype != SDQ_DTYPE_F32 && t->dtype != SDQ_DTYPE_BF16) return SDQ_ERR_CONFIG;
+  s = check_seqs(cache, t->B, t->page_table, t->table_stride, t->max_pages, t->seq_lens, t->max_len, &a.seqs);
   if (s != SDQ_OK) return s;
-  if (!std::isfinite(scale)) return SDQ_ERR_VALUE;
-  if (weight_out && !cache->weight) return SDQ_ERR_NULL;
-  const int64_t elt = dtype == SDQ_DTYPE_F32 ? 4 : 2;
-  if (!heads_fit(cache, heads_q) || !attn_fits(cache, B, heads_q, a.seqs.cap) ||
-      q_stride < int64_t(heads_q) * cache->dim || q_stride > (int64_t(1) << 40) || q_stride * elt % 16)
+  if (!std::isfinite(t->scale)) return SDQ_ERR_VALUE;
+  if (t->weight_out && !cache->weight) return SDQ_ERR_NULL;
+  const int64_t elt = t->dtype == SDQ_DTYPE_F32 ? 4 : 2;
+  if (!heads_fit(cache, t->heads_q) || !attn_fits(cache, t->B, t->heads_q, a.seqs.cap) ||
+      t->q_stride < int64_t(t->heads_q) * cache->dim || t->q_stride > (int64_t(1) << 40) || t->q_stride * elt % 16)
     return SDQ_ERR_SHAPE;
-  if (B == 0) return SDQ_OK;
-  if (!q || !out || !workspace) return SDQ_ERR_NULL;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return SDQ_ERR_SHAPE;
-  if (ws_bytes < attn_decode_workspace_bytes(cache->heads, cache->dim, heads_q, B, a.seqs.cap, weight_out != nullptr))
+  if (t->B == 0) return SDQ_OK;
+  if (!t->q || !t->out || !t->workspace) return SDQ_ERR_NULL;
+  if (!aligned16(t->q) || !aligned16(t->out) || !aligned16(t->workspace)) return SDQ_ERR_SHAPE;
+  if (t->ws_bytes <
+      attn_decode_workspace_bytes(cache->heads, cache->dim, t->heads_q, t->B, a.seqs.cap, t->weight_out != nullptr))
     return SDQ_ERR_BUFFER_TOO_SMALL;
-  a.q = q;
-  a.q_stride = q_stride;
-  a.heads_q = uint32_t(heads_q);
-  a.group = uint32_t(heads_q / cache->heads);
-  a.scale = scale;
-  a.out = out;
-  a.lse = lse;
+  a.q = t->q;
+  a.q_stride = t->q_stride;
+  a.heads_q = uint32_t(t->heads_q);
+  a.group = uint32_t(t->heads_q / cache->heads);
+  a.scale = t->scale;
+  a.out = t->out;
+  a.lse = t->lse;
   a.weight_in = cache->weight;
-  a.weight_out = weight_out;
-  a.ws = static_cast<float*>(workspace);
+  a.weight_out = t->weight_out;
+  a.ws = static_cast<float*>(t->workspace);
   drop_pending_error();
-  const hipError_t e = launch_attn_decode(a, dtype == SDQ_DTYPE_F32, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_attn_decode(a, t->dtype == SDQ_DTYPE_F32, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SDQ_OK : SDQ_ERR_HIP;
 }
 
@@ -186,30 +185,27 @@ extern "C" sdq_status sdq_cache_evict_workspace_size(const sdq_kv_cache* cache, 
   return SDQ_OK;
 }
 
-extern "C" sdq_status sdq_cache_evict(const sdq_kv_cache* cache, int64_t B, const int32_t* page_table,
-                                      int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
-                                      int64_t max_len, int64_t budget, int64_t recent, int32_t* lens_out,
-                                      int32_t* position_out, float* weight_out, void* workspace, size_t ws_bytes,
-                                      void* stream) {
+extern "C" sdq_status sdq_cache_evict(const sdq_kv_cache* cache, const sdq_evict_args* t, void* stream) {
   EvictArgs a;
   sdq_status s = check_cache(cache, &a.kv);
   if (s != SDQ_OK) return s;
-  if (!cache->position || !cache->weight) return SDQ_ERR_NULL;
-  s = check_seqs(cache, B, page_table, table_stride, max_pages, seq_lens, max_len, &a.seqs);
+  if (!t || !cache->position || !cache->weight) return SDQ_ERR_NULL;
+  s = check_seqs(cache, t->B, t->page_table, t->table_stride, t->max_pages, t->seq_lens, t->max_len, &a.seqs);
   if (s != SDQ_OK) return s;
-  if (budget < 1 || recent < 0 || recent > budget || B * cache->heads >= (int64_t(1) << 28)) return SDQ_ERR_SHAPE;
-  if (B == 0) return SDQ_OK;
-  if (!lens_out || !position_out || !weight_out || !workspace) return SDQ_ERR_NULL;
-  if ((position_out == cache->position) != (weight_out == cache->weight)) return SDQ_ERR_CONFIG;
-  if (!aligned16(workspace)) return SDQ_ERR_SHAPE;
-  if (ws_bytes < cache_evict_workspace_bytes(cache->heads, B, a.seqs.cap, budget)) return SDQ_ERR_BUFFER_TOO_SMALL;
+  if (t->budget < 1 || t->recent < 0 || t->recent > t->budget || t->B * cache->heads >= (int64_t(1) << 28))
+    return SDQ_ERR_SHAPE;
+  if (t->B == 0) return SDQ_OK;
+  if (!t->lens_out || !t->position_out || !t->weight_out || !t->workspace) return SDQ_ERR_NULL;
+  if ((t->position_out == cache->position) != (t->weight_out == cache->weight)) return SDQ_ERR_CONFIG;
+  if (!aligned16(t->workspace)) return SDQ_ERR_SHAPE;
+  if (t->ws_bytes < cache_evict_workspace_bytes(cache->heads, t->B, a.seqs.cap, t->budget)) return SDQ_ERR_BUFFER_TOO_SMALL;
   // no sequence is longer than the cap
-  a.budget = int32_t(budget < a.seqs.cap ? budget : a.seqs.cap);
-  a.recent = int32_t(recent < a.seqs.cap ? recent : a.seqs.cap);
-  a.lens_out = lens_out;
-  a.position_out = position_out;
-  a.weight_out = weight_out;
-  a.ws = static_cast<int32_t*>(workspace);
+  a.budget = int32_t(t->budget < a.seqs.cap ? t->budget : a.seqs.cap);
+  a.recent = int32_t(t->recent < a.seqs.cap ? t->recent : a.seqs.cap);
+  a.lens_out = t->lens_out;
+  a.position_out = t->position_out;
+  a.weight_out = t->weight_out;
+  a.ws = static_cast<int32_t*>(t->workspace);
   drop_pending_error();
   const hipError_t e = launch_cache_evict(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SDQ_OK : SDQ_ERR_HIP;

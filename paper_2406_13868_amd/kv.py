@@ -15,10 +15,14 @@ import struct
 
 from . import _dev, _lib, _need, _need_bytes, _same_device, _stream, _torch, _workspace, _x_dtype
 
-# sdq_qk_transform as bytes: packing them takes a quarter of the time that
-# filling a ctypes structure does
-_TRANSFORM = struct.Struct("@PPPqiiif")
-assert _TRANSFORM.size == C.sizeof(_lib.sdq_qk_transform)
+# The argument structures as bytes: packing one takes a fraction of the time
+# that filling a ctypes structure, or passing as many arguments, does.
+_APPEND = struct.Struct("@7P3q5if")
+_ATTN = struct.Struct("@7PN5q2if0q")
+_EVICT = struct.Struct("@6PN6q")
+assert _APPEND.size == C.sizeof(_lib.sdq_append_args)
+assert _ATTN.size == C.sizeof(_lib.sdq_attn_args)
+assert _EVICT.size == C.sizeof(_lib.sdq_evict_args)
 
 
 def _ptr(t, shape, dtype, cache, what):
@@ -147,8 +151,7 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
         _same_device(cache.k, qkv)
     dt = _x_dtype(qkv)
     at = _ptr(slot, (M,), torch.int64, cache, "slot")
-    where = qw = kw = angles = None
-    rot = positions = 0
+    where = qw = kw = angles = rot = positions = 0
     if pos is not None:
         where = _ptr(pos, (M,), torch.int32, cache, "pos")
     elif cos_sin is not None or cache.position is not None:
@@ -166,9 +169,9 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     if out is None:
         out = torch.empty((M, heads_q, dim), dtype=out_dtype or qkv.dtype, device=qkv.device)
     to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
-    t = _TRANSFORM.pack(qw or 0, kw or 0, angles if rot else 0, positions, heads_q, rot, interleaved, eps)
-    rc = _lib.lib().sdq_qkv_append(cache._ref, t, qkv.data_ptr(), dt, M, ld if M > 1 else width, where, at, to, _x_dtype(out),
-                                   _stream(stream))
+    rc = _lib.lib().sdq_qkv_append(cache._ref, _APPEND.pack(
+        qkv.data_ptr(), where, at, to, qw, kw, angles if rot else 0, M, ld if M > 1 else width, positions, dt,
+        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), _stream(stream))
     if rc:
         _lib.check(rc, "sdq_qkv_append")
     return out
@@ -209,8 +212,8 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     if out is None:
         out = torch.empty((B, heads_q, dim), dtype=q.dtype, device=q.device)
     to = _ptr(out, (B, heads_q, dim), q.dtype, cache, "out")
-    log = None if lse is None else _ptr(lse, (B, heads_q), torch.float32, cache, "lse")
-    weights = None
+    log = 0 if lse is None else _ptr(lse, (B, heads_q), torch.float32, cache, "lse")
+    weights = 0
     if weight_out is not None:
         if cache.weight is None:
             raise ValueError("weight_out needs a cache that keeps weights")
@@ -219,15 +222,15 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     if max_len is not None and max_len < cap:
         cap = max_len
     if workspace is None:
-        workspace = _workspace(attn_decode_workspace_size(cache, B, heads_q, cap, weights is not None), q.device, stream)
+        workspace = _workspace(attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), q.device, stream)
     elif workspace.get_device() != cache._index:
         _same_device(cache.k, workspace)
-    rc = _lib.lib().sdq_attn_decode(
-        cache._ref, q.data_ptr(), dt, B, heads_q, q_ld if B > 1 else heads_q * dim, table, ld, width, lens, cap,
-        dim ** -0.5 if scale is None else scale, to, log, weights, _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
+    rc = _lib.lib().sdq_attn_decode(cache._ref, _ATTN.pack(
+        q.data_ptr(), table, lens, to, log, weights, _dev(workspace, "workspace"), workspace.nbytes, B,
+        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), _stream(stream))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
-            _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights is not None), "workspace")
+            _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), "workspace")
         _lib.check(rc, "sdq_attn_decode")
     return out
 
@@ -270,8 +273,9 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
         workspace = _workspace(cache_evict_workspace_size(cache, B, cap, budget), cache.device, stream)
     elif workspace.get_device() != cache._index:
         _same_device(cache.k, workspace)
-    rc = _lib.lib().sdq_cache_evict(cache._ref, B, table, ld, width, lens, cap, budget, recent, new, positions, weights,
-                                    _dev(workspace, "workspace"), workspace.nbytes, _stream(stream))
+    rc = _lib.lib().sdq_cache_evict(cache._ref, _EVICT.pack(
+        table, lens, new, positions, weights, _dev(workspace, "workspace"), workspace.nbytes, B, ld, width, cap, budget, recent),
+        _stream(stream))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, cache_evict_workspace_size(cache, B, cap, budget), "workspace")

@@ -18,21 +18,29 @@ def _cache(**kw):
     return _lib.sdq_kv_cache(**(f | kw))
 
 
-def _append(cache=None, t=None, qkv=P, x=0, M=1, ld=24 * 64, pos=P, slot=P, out=P, qd=0, **kw):
-    f = dict(q_weight=None, k_weight=None, cos_sin=P, positions=10, heads_q=8, rot_dim=64, interleaved=0, eps=1e-6)
-    t = _lib.sdq_qk_transform(**(f | (t or {})))
-    return _lib.lib().sdq_qkv_append(C.byref(cache or _cache(**kw)), C.byref(t), qkv, x, M, ld, pos, slot, out, qd, None)
+def _append(t=None, qkv=P, x=0, M=1, ld=24 * 64, pos=P, slot=P, out=P, qd=0, **kw):
+    f = dict(qkv=qkv, pos=pos, slot=slot, q_out=out, q_weight=None, k_weight=None, cos_sin=P, M=M, row_stride=ld, positions=10, x_dtype=x,
+             q_dtype=qd, heads_q=8, rot_dim=64, interleaved=0, eps=1e-6)
+    return _lib.lib().sdq_qkv_append(C.byref(_cache(**kw)), C.byref(_lib.sdq_append_args(**(f | (t or {})))), None)
 
 
-def _attend(cache=None, q=P, qt=0, B=2, hq=8, qs=8 * 64, table=P, ts=4, mp=4, lens=P, max_len=64, scale=1.0, out=P, lse=None,
-            w=None, ws=P, nbytes=1 << 40, **kw):
-    return _lib.lib().sdq_attn_decode(C.byref(cache or _cache(**kw)), q, qt, B, hq, qs, table, ts, mp, lens, max_len, scale, out, lse,
-                                      w, ws, nbytes, None)
+def _attend(q=P, qt=0, B=2, hq=8, qs=8 * 64, table=P, ts=4, mp=4, lens=P, max_len=64, scale=1.0, out=P, lse=None, w=None, ws=P,
+            nbytes=1 << 40, **kw):
+    t = _lib.sdq_attn_args(q=q, page_table=table, seq_lens=lens, out=out, lse=lse, weight_out=w, workspace=ws, ws_bytes=nbytes, B=B,
+                           q_stride=qs, table_stride=ts, max_pages=mp, max_len=max_len, dtype=qt, heads_q=hq, scale=scale)
+    return _lib.lib().sdq_attn_decode(C.byref(_cache(**kw)), C.byref(t), None)
 
 
-def _evict(cache=None, B=2, table=P, ts=4, mp=4, lens=P, max_len=64, budget=8, recent=2, lo=P, po=P, wo=P, ws=P, nbytes=1 << 40, **kw):
-    c = cache or _cache(**(dict(position=P, weight=P) | kw))
-    return _lib.lib().sdq_cache_evict(C.byref(c), B, table, ts, mp, lens, max_len, budget, recent, lo, po, wo, ws, nbytes, None)
+def _evict(B=2, table=P, ts=4, mp=4, lens=P, max_len=64, budget=8, recent=2, lo=P, po=P, wo=P, ws=P, nbytes=1 << 40, **kw):
+    t = _lib.sdq_evict_args(page_table=table, seq_lens=lens, lens_out=lo, position_out=po, weight_out=wo, workspace=ws, ws_bytes=nbytes,
+                            B=B, table_stride=ts, max_pages=mp, max_len=max_len, budget=budget, recent=recent)
+    return _lib.lib().sdq_cache_evict(C.byref(_cache(**(dict(position=P, weight=P) | kw))), C.byref(t), None)
+
+
+def test_null_arguments():
+    L, c = _lib.lib(), C.byref(_cache(position=P, weight=P))
+    for f in (L.sdq_qkv_append, L.sdq_attn_decode, L.sdq_cache_evict):
+        assert f(c, None, None) == NULL and f(None, None, None) == NULL
 
 
 NULL, SHAPE, CONFIG, SMALL, VALUE = -1, -2, -3, -4, -7
