@@ -67,8 +67,8 @@ def evict(weight, position, budget: int, recent: int):
     if n <= budget:
         return np.zeros(0, int), np.zeros(0, int), weight.copy(), position.copy()
     newest = max(-1, int(position.max()))
-    slots = sorted(range(n), key=lambda t: (not position[t] > newest - recent,
-                                            math.inf if math.isnan(weight[t]) else -float(weight[t]), t))
+    slots = sorted(range(n), key=lambda t: (not position[t] > newest - recent, math.isnan(weight[t]),
+                                            0.0 if math.isnan(weight[t]) else -float(weight[t]), t))
     kept = set(slots[:budget])
     to = np.array([t for t in range(budget) if t not in kept], int)
     of = np.array([t for t in range(budget, n) if t in kept], int)

@@ -15,7 +15,8 @@
 // Up to 16384 slots are read once and kept in registers (1, 4, 8 or 16 per thread,
 // the fewest that hold max_len); beyond, every pass reads them again from the L2,
 // eight per thread at a time.
-// A second kernel moves the rows, 16 bytes per lane.
+// It moves the rows too where that is the faster way; otherwise a second kernel
+// does, 16 bytes per lane.
 #include <hip/hip_runtime.h>
 
 #include "kv_cache.h"
@@ -94,14 +95,55 @@ __device__ __forceinline__ void scan_table(uint32_t* table, int steps, uint32_t*
   __syncthreads();
 }
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// Rows pass through once: loads and stores leave the caches to others (32 x 8192
+// slots 515 us, without the hint 525).
+__device__ __forceinline__ u32x4 stream_load(const uint8_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+}
+__device__ __forceinline__ void stream_store(uint8_t* p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+}
+
+// Moves first + i, first + i + step, ... of the list, i being the thread's index
+// over 2^lpr_log.
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, int count, const int32_t* table, uint32_t h,
+                                          int lpr_log, int first, int step) {
+  const int lane = threadIdx.x & ((1 << lpr_log) - 1);
+  const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
+  for (int i = first + int(threadIdx.x >> lpr_log); i < count; i += step) {
+    const int2 move = list[i];
+    const uint32_t tp = a.kv.per_page.div(move.x), fp = a.kv.per_page.div(move.y);
+    const uint32_t tpage = uint32_t(table[tp]), fpage = uint32_t(table[fp]);
+    if (tpage >= a.kv.pages || fpage >= a.kv.pages) continue;
+    const uint32_t toff = move.x - tp * a.kv.page_size, foff = move.y - fp * a.kv.page_size;
+    const int64_t dst = tpage * a.kv.page_stride + h * a.kv.head_stride + toff * a.kv.slot_stride;
+    const int64_t src = fpage * a.kv.page_stride + h * a.kv.head_stride + foff * a.kv.slot_stride;
+    if (lane * 16u < bytes) {
+      const u32x4 k = stream_load(a.kv.k + src + lane * 16);
+      const u32x4 v = stream_load(a.kv.v + src + lane * 16);
+      stream_store(a.kv.k + dst + lane * 16, k);
+      stream_store(a.kv.v + dst + lane * 16, v);
+    }
+    if (a.kv.e4m3 && lane == 0) {
+      const int64_t ts = (int64_t(tpage) * a.kv.heads + h) * a.kv.page_size + toff;
+      const int64_t fs = (int64_t(fpage) * a.kv.heads + h) * a.kv.page_size + foff;
+      a.kv.k_scale[ts] = a.kv.k_scale[fs];
+      a.kv.v_scale[ts] = a.kv.v_scale[fs];
+    }
+  }
+}
+
 // lists: per row the number of moves, the new length, and `most` pairs of a
-// destination and a source.  The new lengths reach lens_out from the second
-// kernel: it may be seq_lens, which the workgroups of the other heads still read
+// destination and a source.  `alone`: the workgroup moves its rows itself and
+// writes the new length.  Otherwise both are the second kernel's, which is also
+// where lens_out is seq_lens: the workgroups of the other heads still read it
 // here.
 // KEEP: slots per thread kept in registers; 0: read again in every pass.  Up to
 // 8 the registers leave room for two workgroups on a compute unit.
 template <int KEEP>
-__global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, int2* lists, int most) {
+__global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, int2* lists, int most, bool alone, int lpr_log) {
   __shared__ uint32_t hist[3][kDigits];
   __shared__ uint32_t table[(KEEP ? KEEP : 8) * kWaves];
   __shared__ uint32_t waves[7][kWaves];
@@ -112,6 +154,7 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
   const Slots slots{a.kv, a.seqs.table + b * a.seqs.stride, uint32_t(row - b * int(a.kv.heads))};
   int2* list = lists + int64_t(row) * (1 + most);
   const bool in_place = a.weight_out == a.kv.weight;
+  if (alone && tid == 0 && slots.h == 0) a.lens_out[b] = keep;
   if (n <= keep) {
     if (tid == 0) list[0] = make_int2(0, keep);
     if (!in_place)
@@ -312,48 +355,21 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
     if constexpr (KEEP == 0) __syncthreads();  // the next steps write the table
   });
   if (tid == 0) list[0] = make_int2(int(n_moves), keep);
+  if (alone) {
+    __syncthreads();
+    move_rows(a, list + 1, int(n_moves), slots.table, slots.h, lpr_log, 0, kSelect >> lpr_log);
+  }
 }
 
-// Moves of a row: LPR lanes of 16 bytes per key and value.
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-// Rows pass through once: loads and stores leave the caches to others (32 x 8192
-// slots 515 us, without the hint 525).
-__device__ __forceinline__ u32x4 stream_load(const uint8_t* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-}
-__device__ __forceinline__ void stream_store(uint8_t* p, u32x4 v) {
-  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
-}
-template <int LPR>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, const int2* lists, int most, int per_row) {
-  const int row = blockIdx.x / per_row, part = blockIdx.x - row * per_row;
+// 2^lpr_log lanes of 16 bytes per key and value: the smallest that hold a row.
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, const int2* lists, int most, int per_row, int lpr_log) {
+  const int row = blockIdx.x / per_row, part = blockIdx.x - row * per_row, b = row / int(a.kv.heads);
+  const uint32_t h = row - b * int(a.kv.heads);
   const int2* list = lists + int64_t(row) * (1 + most);
   const int2 head = list[0];
-  const int count = head.x, b = row / int(a.kv.heads), lane = threadIdx.x % LPR;
-  const uint32_t h = row - b * int(a.kv.heads), bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
   if (h == 0 && part == 0 && threadIdx.x == 0) a.lens_out[b] = head.y;
-  const int32_t* table = a.seqs.table + b * a.seqs.stride;
-  for (int i = part * (256 / LPR) + threadIdx.x / LPR; i < count; i += per_row * (256 / LPR)) {
-    const int2 move = list[1 + i];
-    const uint32_t tp = a.kv.per_page.div(move.x), fp = a.kv.per_page.div(move.y);
-    const uint32_t tpage = uint32_t(table[tp]), fpage = uint32_t(table[fp]);
-    if (tpage >= a.kv.pages || fpage >= a.kv.pages) continue;
-    const uint32_t toff = move.x - tp * a.kv.page_size, foff = move.y - fp * a.kv.page_size;
-    const int64_t dst = tpage * a.kv.page_stride + h * a.kv.head_stride + toff * a.kv.slot_stride;
-    const int64_t src = fpage * a.kv.page_stride + h * a.kv.head_stride + foff * a.kv.slot_stride;
-    if (lane * 16u < bytes) {
-      const u32x4 k = stream_load(a.kv.k + src + lane * 16);
-      const u32x4 v = stream_load(a.kv.v + src + lane * 16);
-      stream_store(a.kv.k + dst + lane * 16, k);
-      stream_store(a.kv.v + dst + lane * 16, v);
-    }
-    if (a.kv.e4m3 && lane == 0) {
-      const int64_t ts = (int64_t(tpage) * a.kv.heads + h) * a.kv.page_size + toff;
-      const int64_t fs = (int64_t(fpage) * a.kv.heads + h) * a.kv.page_size + foff;
-      a.kv.k_scale[ts] = a.kv.k_scale[fs];
-      a.kv.v_scale[ts] = a.kv.v_scale[fs];
-    }
-  }
+  const int per_block = 256 >> lpr_log;
+  move_rows(a, list + 1, head.x, a.seqs.table + b * a.seqs.stride, h, lpr_log, part * per_block, per_row * per_block);
 }
 
 // Moves of one row, at most.
@@ -371,23 +387,26 @@ size_t cache_evict_workspace_bytes(uint32_t heads_kv, int64_t B, int64_t cap, in
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   int2* const ws = reinterpret_cast<int2*>(a.ws);
   const int most = int(most_moves(a.seqs.cap, a.budget)), rows = a.seqs.B * int(a.kv.heads);
-  if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, ws, most);
-  else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most);
-  else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most);
-  else if (a.seqs.cap <= 16 * kSelect) evict_select_kernel<16><<<rows, kSelect, 0, st>>>(a, ws, most);
-  else evict_select_kernel<0><<<rows, kSelect, 0, st>>>(a, ws, most);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
   const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
-  const int lpr = bytes <= 128 ? 8 : bytes <= 256 ? 16 : 32, per_block = 256 / lpr;
+  const int lpr_log = bytes <= 128 ? 3 : bytes <= 256 ? 4 : 5, per_block = 256 >> lpr_log;
+  // Few moves per row cost less than a second launch (16 x 8 rows of 2000 slots, at
+  // most 128 moves: 17.1 us, with one 17.7; 256: 21.0 and 20.7, and the host issues
+  // one launch less; 512: 27.1 and 24.7), and where there are workgroups for two
+  // rounds, some select while others move (32 x 32 rows of 8192 slots, 4096 moves:
+  // 496 us, with a second launch 511).
+  const bool alone = (most <= 256 || rows >= 1024) && a.lens_out != a.seqs.lens;
+  if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  else if (a.seqs.cap <= 16 * kSelect) evict_select_kernel<16><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  else evict_select_kernel<0><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || alone) return e;
   int per_row = most > 0 ? (most + per_block - 1) / per_block : 1;
   // rows enough to fill the GPU take fewer workgroups each
   const int fill = (256 * 16 + rows - 1) / rows;
   if (per_row > fill) per_row = fill;
-  const dim3 grid(uint32_t(rows) * per_row);
-  if (lpr == 8) evict_move_kernel<8><<<grid, 256, 0, st>>>(a, ws, most, per_row);
-  else if (lpr == 16) evict_move_kernel<16><<<grid, 256, 0, st>>>(a, ws, most, per_row);
-  else evict_move_kernel<32><<<grid, 256, 0, st>>>(a, ws, most, per_row);
+  evict_move_kernel<<<uint32_t(rows) * per_row, 256, 0, st>>>(a, ws, most, per_row, lpr_log);
   return hipGetLastError();
 }
 

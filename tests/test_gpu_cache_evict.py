@@ -20,6 +20,9 @@ CASES = [
     ([2500, 40], 1, 256, 48, "bf16", "wide", 1100, 33, "odd"),
     ([5000], 2, 32, 128, "bf16", "hnd", 4999, 5, "spread"),
     ([5000], 2, 32, 128, "bf16", "hnd", 1, 0, "few"),
+    ([600] * 30 + [301, 299], 32, 16, 16, "bf16", "hnd", 300, 7, "spread"),  # more rows than compute units hold at once
+    ([17000, 12000], 1, 16, 256, "e4m3", "hnd", 9000, 50, "few"),  # more slots than stay in registers, ties across batches
+    ([9000], 1, 16, 33, "bf16", "hnd", 8900, 500, "odd"),
 ]
 
 

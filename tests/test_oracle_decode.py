@@ -66,3 +66,8 @@ def test_eviction_ties_go_to_the_lowest_slot_and_nan_is_lowest():
     w = np.array([1, np.nan, 1, 1, 0, 1], np.float32)
     of, to, w2, p2 = O.evict(w, np.arange(6, dtype=np.int32), 3, 0)
     assert list(to) == [1] and list(of) == [3] and list(p2) == [0, 3, 2, -1, -1, -1]
+
+
+def test_eviction_keeps_minus_infinity_before_nan():
+    of, to, w2, p2 = O.evict(np.array([np.nan, -np.inf, 1], np.float32), np.arange(3, dtype=np.int32), 2, 0)
+    assert list(to) == [0] and list(of) == [2] and list(p2) == [2, 1, -1]
