@@ -15,6 +15,9 @@
 // other a partial result (maximum, sum and unnormalized output of each head)
 // goes to the workspace, and a second kernel joins the partials of each row
 // in the order of their workgroups, so that results do not depend on timing.
+// (Joined by the last workgroup of a row to finish instead, the write-back and
+// invalidation of the L2s that such a handover takes cost more than the launch:
+// one sequence of 4000 slots, 32/8 heads, 54 us against 12.)
 //
 // Matrix instructions (16x16x32 bf16).  Scores: A = 16 keys, B =
 // the row's query heads.  The score of 16 keys x 16 heads leaves each lane 4
@@ -64,7 +67,8 @@ struct Plan {
   uint32_t head;      // what a row costs beside its chunks, in chunks
   bool whole;         // rows are not split
   int64_t score_ld;   // floats between the scores of two query heads
-  float* part;        // [groups][2][gh * (dim + 2)]: m[gh], l[gh], o[gh][dim]
+  uint32_t part_ld;   // floats per partial result: o[gh][dim], m[gh], l[gh], in whole cache lines
+  float* part;        // [groups][2][part_ld]
   float* lse2;        // [B][heads_q]: log2 of the sum, for the rows finished in one workgroup
   float* scores;      // [B][heads_q][score_ld], log2 units; tracked calls only
 };
@@ -200,6 +204,110 @@ __device__ __forceinline__ void request_1k(__amdgpu_buffer_rsrc_t from, uint8_t*
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Where the partials of a row lie: those of workgroups w0 to w1, in order.
+struct RowParts {
+  int w0, w1, row_first;
+  // first: of the row's chunks
+  __device__ __forceinline__ RowParts(const Ranges& ranges, int first, int chunks)
+      : w0(ranges.owner(first)), w1(ranges.owner(first + chunks - 1)), row_first(first) {}
+  __device__ __forceinline__ static RowParts of(const Chunks& all, const Ranges& ranges, int b, int row) {
+    const int chunks = chunks_of(seq_len(all.s, b), all.cl);
+    return RowParts(ranges, all.first_of(b) + row * (all.head + chunks) + all.head, chunks);
+  }
+  __device__ __forceinline__ const float* part(const Plan& p, const Ranges& ranges, int w) const {
+    return p.part + (int64_t(w) * 2 + (row_first >= ranges.start(w) ? 1 : 0)) * p.part_ld;
+  }
+};
+
+// Maximum and sum of a head of a split row, by one wave.
+__device__ __forceinline__ void head_stats(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp,
+                                           int h, int lane, float& top, float& sum) {
+  top = kNegInf;
+  for (int w = rp.w0 + lane; w <= rp.w1; w += 64) top = fmaxf(top, rp.part(p, ranges, w)[p.gh * a.kv.dim + h]);
+#pragma unroll
+  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  const float ref = top == kNegInf ? 0.f : top;
+  sum = 0.f;
+  for (int w = rp.w0 + lane; w <= rp.w1; w += 64) {
+    const float* part = rp.part(p, ranges, w) + p.gh * a.kv.dim;
+    sum += __builtin_amdgcn_exp2f(part[h] - ref) * part[p.gh + h];
+  }
+#pragma unroll
+  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+}
+
+// Outputs of query heads qh0 .. qh0 + heads - 1 (heads h0 .. of their row) from the
+// parts of the row, by the whole workgroup.  dim / 4 threads per head and set of
+// parts; each set joins its own as they arrive, four requested at a time, and the
+// sets meet in shared memory (sm: 1024 floats, sm_ml: 128).
+template <bool F32>
+__device__ __forceinline__ void join_heads(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp, int64_t qh0,
+                                           int h0, int heads, float* sm, float* sm_ml) {
+  const uint32_t D = a.kv.dim;
+  const int per = int(D) / 4, groups = 256 / per, group = threadIdx.x / per, d = (threadIdx.x - group * per) * 4;
+  for (int base = 0; base < heads; base += groups) {
+    const int n = min(heads - base, groups), sets = groups / n, h = group % n, set = group / n;
+    const bool mine = group < n * sets;
+    float top = kNegInf, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
+    if (mine)
+      for (int w = rp.w0 + set; w <= rp.w1; w += 4 * sets) {
+        float pm[4], pl[4];
+        float4 po[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bool in = w + k * sets <= rp.w1;
+          const float* part = rp.part(p, ranges, in ? w + k * sets : w);
+          pm[k] = in ? part[p.gh * D + h0 + base + h] : kNegInf;
+          pl[k] = part[p.gh * D + p.gh + h0 + base + h];
+          po[k] = *reinterpret_cast<const float4*>(part + (h0 + base + h) * D + d);
+        }
+        const float t = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), top), ref = t == kNegInf ? 0.f : t;
+        const float old = __builtin_amdgcn_exp2f(top - ref);
+        sum *= old;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r[x] *= old;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
+          sum += f * pl[k];
+          r[0] += f * po[k].x;
+          r[1] += f * po[k].y;
+          r[2] += f * po[k].z;
+          r[3] += f * po[k].w;
+        }
+        top = t;
+      }
+    __syncthreads();  // what the shared memory held has been read
+    *reinterpret_cast<float4*>(&sm[threadIdx.x * 4]) = make_float4(r[0], r[1], r[2], r[3]);
+    if (d == 0 && mine) {
+      sm_ml[group] = top;
+      sm_ml[64 + group] = sum;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * int(D); i += 256) {
+      const int hh = i / int(D), x = i - hh * int(D);
+      float most = kNegInf;
+      for (int k = 0; k < sets; ++k) most = fmaxf(most, sm_ml[k * n + hh]);
+      const float ref = most == kNegInf ? 0.f : most;
+      float total = 0.f, y = 0.f;
+      for (int k = 0; k < sets; ++k) {
+        const float f = __builtin_amdgcn_exp2f(sm_ml[k * n + hh] - ref);
+        total += f * sm_ml[64 + k * n + hh];
+        y += f * sm[(k * n + hh) * int(D) + x];
+      }
+      const int64_t qh = qh0 + base + hh;
+      y *= total == 0.f ? 0.f : 1.f / total;
+      if constexpr (F32) static_cast<float*>(a.out)[qh * D + x] = y;
+      else static_cast<__bf16*>(a.out)[qh * D + x] = static_cast<__bf16>(y);
+      if (x == 0) {
+        const float lse2 = most + __log2f(total);
+        p.lse2[qh] = lse2;
+        if (a.lse) a.lse[qh] = lse2 * kLn2;
+      }
+    }
+  }
 }
 
 // The dimension of value product j in row c: VPL = DP / 16 neighbouring ones per
@@ -578,7 +686,7 @@ __global__ __launch_bounds__(256, occupancy(DP, F32, P16)) void attn_decode_kern
     }
     __syncthreads();
     const bool whole = nc == chunks;
-    float* part = p.part + (int64_t(w) * 2 + (row_at + all.head >= begin ? 1 : 0)) * (p.gh * (D + 2));
+    float* part = p.part + (int64_t(w) * 2 + (row_at + all.head >= begin ? 1 : 0)) * p.part_ld;
     const int per = int(D) / 4;
     for (int i = threadIdx.x; i < heads * per; i += 256) {
       const int h = i / per, d = (i - h * per) * 4;
@@ -613,48 +721,15 @@ __global__ __launch_bounds__(256, occupancy(DP, F32, P16)) void attn_decode_kern
         }
       } else {
         if (d == 0) {
-          part[h] = top;
-          part[p.gh + h] = sum;
+          part[p.gh * D + h] = top;
+          part[p.gh * D + p.gh + h] = sum;
         }
-        float* po = part + 2 * p.gh + h * D + d;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) po[x] = r[x];
+        *reinterpret_cast<float4*>(part + h * D + d) = make_float4(r[0], r[1], r[2], r[3]);
       }
     }
     __syncthreads();
     at = row_end;
   }
-}
-
-// Where the partials of a row lie: those of workgroups w0 to w1, in order.
-struct RowParts {
-  int w0, w1, row_first;
-  __device__ __forceinline__ RowParts(const Chunks& all, const Ranges& ranges, int b, int row) {
-    const int chunks = chunks_of(seq_len(all.s, b), all.cl);
-    row_first = all.first_of(b) + row * (all.head + chunks) + all.head;  // of its chunks
-    w0 = ranges.owner(row_first);
-    w1 = ranges.owner(row_first + chunks - 1);
-  }
-  __device__ __forceinline__ const float* part(const AttnArgs& a, const Plan& p, const Ranges& ranges, int w) const {
-    return p.part + (int64_t(w) * 2 + (row_first >= ranges.start(w) ? 1 : 0)) * (p.gh * (a.kv.dim + 2));
-  }
-};
-
-// Maximum and sum of a head of a split row, by one wave.
-__device__ __forceinline__ void head_stats(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp,
-                                           int h, int lane, float& top, float& sum) {
-  top = kNegInf;
-  for (int w = rp.w0 + lane; w <= rp.w1; w += 64) top = fmaxf(top, rp.part(a, p, ranges, w)[h]);
-#pragma unroll
-  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-  const float ref = top == kNegInf ? 0.f : top;
-  sum = 0.f;
-  for (int w = rp.w0 + lane; w <= rp.w1; w += 64) {
-    const float* part = rp.part(a, p, ranges, w);
-    sum += __builtin_amdgcn_exp2f(part[h] - ref) * part[p.gh + h];
-  }
-#pragma unroll
-  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
 }
 
 constexpr int kSlotBlock = 1024;  // slots whose weights a workgroup sums
@@ -665,67 +740,17 @@ constexpr int kSlotBlock = 1024;  // slots whose weights a workgroup sums
 template <bool F32>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan p, int joins, int slot_blocks) {
   __shared__ __attribute__((aligned(16))) float sm[256 * 4];
-  __shared__ float sm_m[64], sm_l[64];
+  __shared__ float sm_ml[128];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t D = a.kv.dim;
   const Chunks all(a.seqs, p, lane);
   const Ranges ranges(all.total, p.groups);
   int id = blockIdx.x;
   if (id < joins) {
     const int b = id / int(a.heads_q), hq = id - b * int(a.heads_q), hk = hq / int(a.group), gi = (hq - hk * int(a.group)) / 16;
     const int h = hq - hk * int(a.group) - gi * 16;
-    const RowParts rp(all, ranges, b, hk * int(p.hgroups) + gi);
+    const RowParts rp = RowParts::of(all, ranges, b, hk * int(p.hgroups) + gi);
     if (rp.w0 == rp.w1) return;  // the row was finished in one workgroup
-    // dim / 4 threads per partial, as many partials at a time as fit; each set
-    // of threads joins its own as they arrive, four requested at a time
-    const int per = int(D) / 4, sets = 256 / per, set = threadIdx.x / per, d = (threadIdx.x - set * per) * 4;
-    float top = kNegInf, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (set < sets)
-      for (int w = rp.w0 + set; w <= rp.w1; w += 4 * sets) {
-        float pm[4], pl[4], po[4][4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const bool in = w + k * sets <= rp.w1;
-          const float* part = rp.part(a, p, ranges, in ? w + k * sets : w);
-          pm[k] = in ? part[h] : kNegInf;
-          pl[k] = part[p.gh + h];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) po[k][x] = part[2 * p.gh + h * D + d + x];
-        }
-        const float t = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), top), ref = t == kNegInf ? 0.f : t;
-        const float old = __builtin_amdgcn_exp2f(top - ref);
-        sum *= old;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) r[x] *= old;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
-          sum += f * pl[k];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) r[x] += f * po[k][x];
-        }
-        top = t;
-      }
-    *reinterpret_cast<float4*>(&sm[threadIdx.x * 4]) = make_float4(r[0], r[1], r[2], r[3]);
-    if (d == 0 && set < sets) {
-      sm_m[set] = top;
-      sm_l[set] = sum;
-    }
-    __syncthreads();
-    float most = kNegInf, total = 0.f;
-    for (int k = 0; k < sets; ++k) most = fmaxf(most, sm_m[k]);
-    const float ref = most == kNegInf ? 0.f : most;
-    for (int k = 0; k < sets; ++k) total += __builtin_amdgcn_exp2f(sm_m[k] - ref) * sm_l[k];
-    const int64_t qh = int64_t(b) * a.heads_q + hq;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    for (int x = threadIdx.x; x < int(D); x += 256) {
-      float y = 0.f;
-      for (int k = 0; k < sets; ++k) y += __builtin_amdgcn_exp2f(sm_m[k] - ref) * sm[k * int(D) + x];
-      y *= inv;
-      if constexpr (F32) static_cast<float*>(a.out)[qh * D + x] = y;
-      else static_cast<__bf16*>(a.out)[qh * D + x] = static_cast<__bf16>(y);
-    }
-    if (threadIdx.x == 0 && a.lse) a.lse[qh] = (most + __log2f(total)) * kLn2;
+    join_heads<F32>(a, p, ranges, rp, int64_t(b) * a.heads_q + hq, h, 1, sm, sm_ml);
     return;
   }
   id -= joins;
@@ -744,7 +769,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan p, int 
     at[k] = page < a.kv.pages ? (int64_t(page) * a.kv.heads + hk) * a.kv.page_size + (t - pi * a.kv.page_size) : -1;
   }
   for (int gi = 0; gi < int(p.hgroups); ++gi) {
-    const RowParts rp(all, ranges, b, hk * int(p.hgroups) + gi);
+    const RowParts rp = RowParts::of(all, ranges, b, hk * int(p.hgroups) + gi);
     const int heads = min(16, int(a.group) - gi * 16);
     const int64_t qh = int64_t(b) * a.heads_q + hk * a.group + gi * 16;
     for (int h0 = 0; h0 < heads; h0 += kHeads) {
@@ -792,6 +817,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan p, int 
 struct Sizes {
   uint32_t hgroups, gh;
   int64_t score_ld;
+  uint32_t part_ld;
   size_t part, lse2, scores;  // floats
 };
 Sizes sizes_of(uint32_t heads_kv, uint32_t dim, uint32_t heads_q, int64_t B, int64_t cap, bool track) {
@@ -801,7 +827,8 @@ Sizes sizes_of(uint32_t heads_kv, uint32_t dim, uint32_t heads_q, int64_t B, int
   s.gh = group < 16 ? group : 16;
   s.score_ld = (cap + 63) / 64 * 64;  // whole tiles
   const auto up = [](size_t n) { return (n + 3) / 4 * 4; };
-  s.part = up(size_t(kMostGroups) * 2 * s.gh * (dim + 2));
+  s.part_ld = (s.gh * (dim + 2) + 31) / 32 * 32;  // whole cache lines
+  s.part = size_t(kMostGroups) * 2 * s.part_ld;
   s.lse2 = up(size_t(B) * heads_q);
   s.scores = track ? size_t(B) * heads_q * size_t(s.score_ld) : 0;
   return s;
@@ -863,6 +890,7 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool f32, hipStream_t st) {
   p.part = a.ws;
   p.lse2 = p.part + s.part;
   p.scores = track ? p.lse2 + s.lse2 : nullptr;
+  p.part_ld = s.part_ld;
   if (a.kv.e4m3) {
     if (f32) launch_dim<true, true>(a, p, st);
     else launch_dim<true, false>(a, p, st);
