@@ -221,19 +221,21 @@ struct RowParts {
   }
 };
 
-// Maximum and sum of a head of a split row, by one wave.
+// Maximum and sum of a head of a split row, by one wave: each lane joins its
+// parts as they arrive, then the lanes meet.
 __device__ __forceinline__ void head_stats(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp,
                                            int h, int lane, float& top, float& sum) {
-  top = kNegInf;
-  for (int w = rp.w0 + lane; w <= rp.w1; w += 64) top = fmaxf(top, rp.part(p, ranges, w)[p.gh * a.kv.dim + h]);
-#pragma unroll
-  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-  const float ref = top == kNegInf ? 0.f : top;
-  sum = 0.f;
+  float m = kNegInf, l = 0.f;
   for (int w = rp.w0 + lane; w <= rp.w1; w += 64) {
     const float* part = rp.part(p, ranges, w) + p.gh * a.kv.dim;
-    sum += __builtin_amdgcn_exp2f(part[h] - ref) * part[p.gh + h];
+    const float pm = part[h], pl = part[p.gh + h], t = fmaxf(m, pm), ref = t == kNegInf ? 0.f : t;
+    l = l * __builtin_amdgcn_exp2f(m - ref) + pl * __builtin_amdgcn_exp2f(pm - ref);
+    m = t;
   }
+  top = m;
+#pragma unroll
+  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  sum = l * __builtin_amdgcn_exp2f(m - (top == kNegInf ? 0.f : top));
 #pragma unroll
   for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
 }

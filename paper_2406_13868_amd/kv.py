@@ -13,7 +13,7 @@ from __future__ import annotations
 import ctypes as C
 import struct
 
-from . import _dev, _lib, _need, _need_bytes, _same_device, _stream, _torch, _workspace, _x_dtype
+from . import _dev, _lib, _need, _need_bytes, _same_device, _torch, _workspace, _x_dtype
 
 # The argument structures as bytes: packing one takes a fraction of the time
 # that filling a ctypes structure, or passing as many arguments, does.
@@ -23,6 +23,16 @@ _EVICT = struct.Struct("@6PN6q")
 assert _APPEND.size == C.sizeof(_lib.sdq_append_args)
 assert _ATTN.size == C.sizeof(_lib.sdq_attn_args)
 assert _EVICT.size == C.sizeof(_lib.sdq_evict_args)
+
+
+def _stream(stream, cache, torch):
+    """The stream to run on: the given one, or the current one of the cache's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    try:
+        return torch._C._cuda_getCurrentRawStream(cache._index)
+    except AttributeError:
+        return torch.cuda.current_stream(cache.device).cuda_stream
 
 
 def _ptr(t, shape, dtype, cache, what):
@@ -115,9 +125,9 @@ def _no_overlap(shape, stride):
 
 def _seqs(cache, page_table, seq_lens, torch):
     """Of the page table: B, its width, its row stride and its address; the address of seq_lens."""
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.dtype is not torch.int32:
+    if not isinstance(page_table, torch.Tensor) or page_table.dtype is not torch.int32 or len(shape := page_table.shape) != 2:
         raise ValueError("page_table must be [sequences, pages] int32")
-    B, width = page_table.shape
+    B, width = shape
     lens = _ptr(seq_lens, (B,), torch.int32, cache, "seq_lens")
     ld, step = page_table.stride()
     if step != 1 and width > 1:
@@ -138,9 +148,9 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     [positions, rot_dim], cosines then sines.  Queries have out_dtype, by
     default qkv's."""
     torch = _torch()
-    if not isinstance(qkv, torch.Tensor) or qkv.dim() != 2:
+    if not isinstance(qkv, torch.Tensor) or len(shape := qkv.shape) != 2:
         raise ValueError("qkv must be [M, (heads_q + 2 heads) * dim]")
-    M, width = qkv.shape
+    M, width = shape
     dim = cache.dim
     if heads_q < 1 or width != (heads_q + 2 * cache.heads) * dim:
         raise ValueError(f"qkv must be [M, {(heads_q + 2 * cache.heads) * dim}], got {list(qkv.shape)}")
@@ -169,9 +179,9 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     if out is None:
         out = torch.empty((M, heads_q, dim), dtype=out_dtype or qkv.dtype, device=qkv.device)
     to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
-    rc = _lib.lib().sdq_qkv_append(cache._ref, _APPEND.pack(
+    rc = (_lib._lib or _lib.lib()).sdq_qkv_append(cache._ref, _APPEND.pack(
         qkv.data_ptr(), where, at, to, qw, kw, angles if rot else 0, M, ld if M > 1 else width, positions, dt,
-        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), _stream(stream))
+        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), _stream(stream, cache, torch))
     if rc:
         _lib.check(rc, "sdq_qkv_append")
     return out
@@ -200,9 +210,9 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     torch = _torch()
     B, width, ld, table, lens = _seqs(cache, page_table, seq_lens, torch)
     dim = cache.dim
-    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[0] != B or q.shape[2] != dim:
+    if not isinstance(q, torch.Tensor) or len(shape := q.shape) != 3 or shape[0] != B or shape[2] != dim:
         raise ValueError(f"q must be [{B}, heads_q, {dim}]")
-    heads_q = q.shape[1]
+    heads_q = shape[1]
     dt = _x_dtype(q)
     q_ld, head_ld, step = q.stride()
     if not q.is_cuda or step != 1 or (heads_q > 1 and head_ld != dim):
@@ -211,7 +221,7 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
         _same_device(cache.k, q)
     if out is None:
         out = torch.empty((B, heads_q, dim), dtype=q.dtype, device=q.device)
-    to = _ptr(out, (B, heads_q, dim), q.dtype, cache, "out")
+    to = _ptr(out, shape, q.dtype, cache, "out")
     log = 0 if lse is None else _ptr(lse, (B, heads_q), torch.float32, cache, "lse")
     weights = 0
     if weight_out is not None:
@@ -225,9 +235,9 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
         workspace = _workspace(attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), q.device, stream)
     elif workspace.get_device() != cache._index:
         _same_device(cache.k, workspace)
-    rc = _lib.lib().sdq_attn_decode(cache._ref, _ATTN.pack(
+    rc = (_lib._lib or _lib.lib()).sdq_attn_decode(cache._ref, _ATTN.pack(
         q.data_ptr(), table, lens, to, log, weights, _dev(workspace, "workspace"), workspace.nbytes, B,
-        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), _stream(stream))
+        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), _stream(stream, cache, torch))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), "workspace")
@@ -273,9 +283,9 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
         workspace = _workspace(cache_evict_workspace_size(cache, B, cap, budget), cache.device, stream)
     elif workspace.get_device() != cache._index:
         _same_device(cache.k, workspace)
-    rc = _lib.lib().sdq_cache_evict(cache._ref, _EVICT.pack(
+    rc = (_lib._lib or _lib.lib()).sdq_cache_evict(cache._ref, _EVICT.pack(
         table, lens, new, positions, weights, _dev(workspace, "workspace"), workspace.nbytes, B, ld, width, cap, budget, recent),
-        _stream(stream))
+        _stream(stream, cache, torch))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, cache_evict_workspace_size(cache, B, cap, budget), "workspace")
