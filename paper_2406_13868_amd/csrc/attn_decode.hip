@@ -59,11 +59,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
-constexpr int kMostGroups = 512;  // workgroups, at most
-// Rows of up to this many chunks are not split: a further chunk takes 1.2 us, the
-// second kernel 4 (one sequence of 512 slots, 32 heads: 10.0 us, split 10.3; of 256
-// 7.4 and 9.5; of 700 not split 11.9, 10.7).
-constexpr int kWholeChunks = 4;
+constexpr int kMostGroups = 512;    // workgroups, at most, where rows are split
+constexpr int kWholeGroups = 4096;  // and where they are not
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_huge_valf();
 
@@ -881,7 +878,15 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool f32, hipStream_t st) {
   p.hgroups = s.hgroups;
   p.gh = s.gh;
   p.chunk_log = tile_slots(dim_padded(a.kv.dim), f32) == 64 ? 8 : 7;
-  p.whole = chunks_of(a.seqs.cap, int(p.chunk_log)) <= kWholeChunks;
+  const int64_t rows = int64_t(a.seqs.B) * p.rows, most = chunks_of(a.seqs.cap, int(p.chunk_log));
+  const int row_bytes = dim_padded(a.kv.dim) * (a.kv.e4m3 ? 1 : 2);
+  // Short rows are not split: a further chunk takes 1.2 us (twice that at 512
+  // bytes per slot), the second kernel 4 (one sequence of 512 slots, 32 heads of
+  // 128, bf16: 10.0 us, split 10.3; of 256 7.4 and 9.5; of 700 not split 11.9, 10.7;
+  // 8 heads of 256, 256 slots 10.3 and 11.7, 400 not split 12.7, 11.6).  Nor are
+  // somewhat longer ones where they fill the GPU as they are (32 sequences of 800
+  // e4m3 slots, 8 key heads: 15.1, split 20.8).
+  p.whole = most <= (row_bytes > 256 ? 2 : 4) || (rows >= kMostGroups / 2 && most <= 8);
   // The first loads' latency and the join of the waves take the time of about
   // two chunks; counted, workgroups with many short rows are not the last to
   // finish (64 ragged sequences of up to 8192 e4m3 slots: 351 us, uncounted
@@ -892,10 +897,11 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool f32, hipStream_t st) {
   // results (32 sequences of 1000 slots, 32/8 heads of 128, bf16: 26.0 us, 512
   // workgroups 29.8).  Smaller rows take two (64 sequences of 4096 e4m3 slots:
   // 359 us, 256 workgroups 378).
-  int64_t groups = dim_padded(a.kv.dim) * (a.kv.e4m3 ? 1 : 2) >= 256 ? kMostGroups / 2 : kMostGroups;
-  const int64_t rows = int64_t(a.seqs.B) * p.rows;
+  // Whole rows go to a workgroup each, up to 4096 (128 sequences of up to 300
+  // slots, 16 heads of 64: 26.5 us, 512 workgroups 33.5).
+  int64_t groups = p.whole ? kWholeGroups : row_bytes >= 256 ? kMostGroups / 2 : kMostGroups;
   // no more than there are rows or chunks, or neighbours would be idle
-  groups = std::min(groups, p.whole ? rows : rows * (p.head + chunks_of(a.seqs.cap, int(p.chunk_log))));
+  groups = std::min(groups, p.whole ? rows : rows * (p.head + most));
   p.groups = uint32_t(groups);
   p.score_ld = s.score_ld;
   p.part = a.ws;
