@@ -243,6 +243,12 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    // all of the digit's class stay: no need to look further (a third of the
+    // passes with weights that differ)
+    if (pass > 0 && equal == want) {
+      prefix <<= bits;
+      continue;
+    }
     each([&](int base) {
 #pragma unroll
       for (int k = 0; k < kRegs; ++k) {
