@@ -13,8 +13,9 @@
 // over the weights' bits (three digits, counted in shared memory), then one
 // pass in slot order that settles ties and lists what moves by prefix sums.
 // Up to 16384 slots are read once and kept in registers (1, 4, 8 or 16 per thread,
-// the fewest that hold max_len); beyond, every pass reads them again from the L2,
-// eight per thread at a time.
+// the fewest that hold max_len), up to 32768 in shared memory (one sequence of
+// 31853 slots, 4 key heads: 75 us, read again 107); beyond, every pass reads them
+// again from the L2, eight per thread at a time (40000 slots: 142 us).
 // It moves the rows too where that is the faster way; otherwise a second kernel
 // does, 16 bytes per lane.
 //
@@ -145,10 +146,14 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, 
 // writes the new length.  Otherwise both are the second kernel's, which is also
 // where lens_out is seq_lens: the workgroups of the other heads still read it
 // here.
-// KEEP: slots per thread kept in registers; 0: read again in every pass.  Up to
-// 8 the registers leave room for two workgroups on a compute unit.
-template <int KEEP>
-__global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, int2* lists, int most, bool alone, int lpr_log) {
+// KEEP: slots per thread kept in registers, up to 8 of which leave room for two
+// workgroups on a compute unit.  kShared: 32 of them, the keys in shared memory
+// (in registers they spill).  0: read again in every pass.
+constexpr int kShared = 32;
+template <int SLOTS>
+__global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, int2* lists, int most, bool alone, int lpr_log) {
+  constexpr int KEEP = SLOTS == kShared ? 0 : SLOTS;
+  __shared__ uint32_t key_of[SLOTS == kShared ? kShared : 1][kSelect];  // each thread's own
   __shared__ uint32_t hist[3][kDigits];
   __shared__ uint32_t table[(KEEP ? KEEP : 8) * kWaves];
   __shared__ uint32_t waves[7][kWaves];
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
   constexpr int kRegs = KEEP ? KEEP : 8;
   constexpr int kNone = INT32_MIN;
   uint32_t keys[kRegs];
-  uint32_t recent_bits = 0;
+  uint32_t recent_bits = 0, recent_all = 0;
   int edge = kNone;  // a slot is recent if position > edge
   const auto load = [&](int base, int (&p)[kRegs], bool with_keys) {
 #pragma unroll
@@ -202,9 +207,15 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
       f(0);
     } else {
       for (int base = 0; base < steps; base += kRegs) {
-        int p[kRegs];
-        load(base, p, true);
-        set_recent(p);
+        if constexpr (SLOTS == kShared) {
+#pragma unroll
+          for (int k = 0; k < kRegs; ++k) keys[k] = key_of[base + k][tid];
+          recent_bits = recent_all >> base;
+        } else {
+          int p[kRegs];
+          load(base, p, true);
+          set_recent(p);
+        }
         f(base);
       }
     }
@@ -213,7 +224,26 @@ __global__ __launch_bounds__(kSelect, KEEP && KEEP <= 8 ? 8 : 4) void evict_sele
   for (int i = tid; i < 3 * kDigits; i += kSelect) hist[0][i] = 0;
   int newest = -1;
   uint32_t recents = 0, total;
-  {
+  if constexpr (SLOTS == kShared) {
+    int p[kShared / kRegs][kRegs];
+#pragma unroll
+    for (int g = 0; g < kShared / kRegs; ++g) {
+      load(g * kRegs, p[g], true);
+#pragma unroll
+      for (int k = 0; k < kRegs; ++k) {
+        key_of[g * kRegs + k][tid] = keys[k];
+        newest = max(newest, p[g][k]);
+      }
+    }
+    newest = block_max(newest, waves[0]);
+    edge = int(max(int64_t(newest) - a.recent, int64_t(kNone)));
+#pragma unroll
+    for (int g = 0; g < kShared / kRegs; ++g) {
+      set_recent(p[g]);
+      recent_all |= recent_bits << (g * kRegs);
+    }
+    recents = __popc(recent_all);
+  } else {
     int p[kRegs];
     for (int base = 0; base < steps; base += kRegs) {
       load(base, p, KEEP > 0);
@@ -410,6 +440,7 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 16 * kSelect) evict_select_kernel<16><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
+  else if (a.seqs.cap <= kShared * kSelect) evict_select_kernel<kShared><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else evict_select_kernel<0><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || alone) return e;

@@ -23,6 +23,9 @@ CASES = [
     ([600] * 30 + [301, 299], 32, 16, 16, "bf16", "hnd", 300, 7, "spread"),  # more rows than compute units hold at once
     ([17000, 12000], 1, 16, 256, "e4m3", "hnd", 9000, 50, "few"),  # more slots than stay in registers, ties across batches
     ([9000], 1, 16, 33, "bf16", "hnd", 8900, 500, "odd"),
+    ([31853, 16385, 300], 2, 32, 64, "bf16", "wide", 20000, 4000, "odd"),  # keys in shared memory
+    ([33000, 20000], 1, 16, 256, "e4m3", "hnd", 9000, 50, "few"),  # read again in every pass
+    ([40001], 1, 16, 7, "bf16", "nhd", 39000, 0, "spread"),
 ]
 
 
