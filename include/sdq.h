@@ -553,8 +553,9 @@ sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_append_args* args
  * A sequence without a slot gives zeros and lse = -inf.  Scores, softmax and
  * sums are fp32; the probabilities enter the second product with 17 bits (bf16
  * outputs) or 24 (fp32).  Deterministic.  B = 0 is a no-op; B up to 2^20, with
- * B * heads * ceil(heads_q / heads / 16) * ceil(max_len / 128) and the launches'
- * other counts below 2^31. */
+ * B * heads * ceil(heads_q / heads / 16) * (ceil(max_len / 128) + 8) below
+ * 2^31, and B * heads_q (with weight_out + B * heads * ceil(max_len / 1024))
+ * below 2^24. */
 typedef struct {
   const void* q;
   const int32_t *page_table, *seq_lens;
@@ -588,7 +589,8 @@ sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_args* args,
  *   workspace device, 16-byte aligned, sdq_cache_evict_workspace_size bytes
  * Keys and values move in place; what lies in slots past the new length is not
  * cleared, and pages wholly past it are the caller's again.  Sequences share
- * no page.  1 <= budget, 0 <= recent <= budget.  B = 0 is a no-op. */
+ * no page.  1 <= budget, 0 <= recent <= budget.  B = 0 is a no-op; B up to
+ * 2^20 and B * heads below 2^22. */
 typedef struct {
   const int32_t *page_table, *seq_lens;
   int32_t *lens_out, *position_out;

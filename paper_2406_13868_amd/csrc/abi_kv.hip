@@ -69,12 +69,14 @@ bool heads_fit(const sdq_kv_cache* c, int32_t heads_q) {
   return heads_q >= 1 && heads_q <= 1024 && heads_q % c->heads == 0;
 }
 
-// Whether the chunk, workgroup and score counts of an attention call fit the
-// kernels' 32-bit indexes.
-bool attn_fits(const sdq_kv_cache* c, int64_t B, int32_t heads_q, int64_t cap) {
+// Workgroups of 256 or 1024 threads: the threads of a launch are counted in 32 bits.
+constexpr int64_t kMostBlocks256 = (int64_t(1) << 24) - 1, kMostBlocks1024 = (int64_t(1) << 22) - 1;
+
+// Whether the chunk and workgroup counts of an attention call fit.
+bool attn_fits(const sdq_kv_cache* c, int64_t B, int32_t heads_q, int64_t cap, bool track) {
   const int64_t rows = int64_t(c->heads) * ((heads_q / c->heads + 15) / 16), lim = int64_t(1) << 31;
-  const int64_t chunks = (cap + 127) / 128 + 8, blocks = (cap + 255) / 256;
-  return B * rows < lim / chunks && B * (heads_q + c->heads * blocks) < lim / 2;
+  const int64_t chunks = (cap + 127) / 128 + 8, blocks = track ? (cap + 1023) / 1024 : 0;
+  return B * rows < lim / chunks && B * (heads_q + c->heads * blocks) <= kMostBlocks256;
 }
 
 // An error that an earlier HIP call on this thread left pending is not this
@@ -133,7 +135,7 @@ extern "C" sdq_status sdq_attn_decode_workspace_size(const sdq_kv_cache* cache, 
   if (s != SDQ_OK) return s;
   if (!bytes) return SDQ_ERR_NULL;
   if (B < 0 || B > (int64_t(1) << 20) || max_len < 0 || max_len >= (int64_t(1) << 31) - 4096 || !heads_fit(cache, heads_q) ||
-      !attn_fits(cache, B, heads_q, max_len))
+      !attn_fits(cache, B, heads_q, max_len, track != 0))
     return SDQ_ERR_SHAPE;
   *bytes = attn_decode_workspace_bytes(cache->heads, cache->dim, heads_q, B, max_len, track != 0);
   return SDQ_OK;
@@ -150,7 +152,7 @@ extern "C" sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_
   if (!std::isfinite(t->scale)) return SDQ_ERR_VALUE;
   if (t->weight_out && !cache->weight) return SDQ_ERR_NULL;
   const int64_t elt = t->dtype == SDQ_DTYPE_F32 ? 4 : 2;
-  if (!heads_fit(cache, t->heads_q) || !attn_fits(cache, t->B, t->heads_q, a.seqs.cap) ||
+  if (!heads_fit(cache, t->heads_q) || !attn_fits(cache, t->B, t->heads_q, a.seqs.cap, t->weight_out != nullptr) ||
       t->q_stride < int64_t(t->heads_q) * cache->dim || t->q_stride > (int64_t(1) << 40) || t->q_stride * elt % 16)
     return SDQ_ERR_SHAPE;
   if (t->B == 0) return SDQ_OK;
@@ -179,7 +181,8 @@ extern "C" sdq_status sdq_cache_evict_workspace_size(const sdq_kv_cache* cache, 
   const sdq_status s = check_cache(cache, nullptr);
   if (s != SDQ_OK) return s;
   if (!bytes) return SDQ_ERR_NULL;
-  if (B < 0 || B > (int64_t(1) << 20) || max_len < 0 || max_len >= (int64_t(1) << 31) - 4096 || budget < 1)
+  if (B < 0 || B > (int64_t(1) << 20) || max_len < 0 || max_len >= (int64_t(1) << 31) - 4096 || budget < 1 ||
+      B * cache->heads > kMostBlocks1024)
     return SDQ_ERR_SHAPE;
   *bytes = cache_evict_workspace_bytes(cache->heads, B, max_len, budget);
   return SDQ_OK;
@@ -192,7 +195,7 @@ extern "C" sdq_status sdq_cache_evict(const sdq_kv_cache* cache, const sdq_evict
   if (!t || !cache->position || !cache->weight) return SDQ_ERR_NULL;
   s = check_seqs(cache, t->B, t->page_table, t->table_stride, t->max_pages, t->seq_lens, t->max_len, &a.seqs);
   if (s != SDQ_OK) return s;
-  if (t->budget < 1 || t->recent < 0 || t->recent > t->budget || t->B * cache->heads >= (int64_t(1) << 28))
+  if (t->budget < 1 || t->recent < 0 || t->recent > t->budget || t->B * cache->heads > kMostBlocks1024)
     return SDQ_ERR_SHAPE;
   if (t->B == 0) return SDQ_OK;
   if (!t->lens_out || !t->position_out || !t->weight_out || !t->workspace) return SDQ_ERR_NULL;

@@ -156,3 +156,24 @@ def test_the_binding_checks_the_calls():
     _raises(lambda: sdq.attn_decode(q, c, table, lens[:2]), "seq_lens must be")
     _raises(lambda: sdq.attn_decode(q, c, table, lens), "CUDA")
     _raises(lambda: sdq.cache_evict(c, table, lens.long(), 4), "seq_lens must be")
+
+
+OK = 0
+
+
+@pytest.mark.parametrize("B,heads,heads_q,max_len,track,status", [
+    (1 << 20, 8, 8, 64, 0, OK), (1 << 20, 16, 16, 64, 0, SHAPE), ((1 << 20) + 1, 1, 1, 64, 0, SHAPE),
+    (4096, 32, 32, 100000, 0, OK), (4096, 32, 32, 100000, 1, OK), (4096, 32, 32, 131072, 1, SHAPE),
+    (1 << 14, 32, 32, 1 << 20, 0, SHAPE),
+])
+def test_attention_counts_that_no_launch_holds_are_refused(B, heads, heads_q, max_len, track, status):
+    n = C.c_size_t()
+    c = _cache(heads=heads)
+    assert _lib.lib().sdq_attn_decode_workspace_size(C.byref(c), B, heads_q, max_len, track, C.byref(n)) == status
+
+
+@pytest.mark.parametrize("B,heads,status", [(1 << 20, 3, OK), (1 << 20, 4, SHAPE), (4096, 1023, OK), (4096, 1024, SHAPE)])
+def test_eviction_counts_that_no_launch_holds_are_refused(B, heads, status):
+    n = C.c_size_t()
+    c = _cache(heads=heads)
+    assert _lib.lib().sdq_cache_evict_workspace_size(C.byref(c), B, 64, 8, C.byref(n)) == status
