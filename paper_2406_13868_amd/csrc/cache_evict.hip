@@ -77,14 +77,20 @@ __device__ __forceinline__ int block_max(int v, uint32_t* waves) {
 }
 
 // Where a sequence's slots lie: index into [pages][heads][page_size], -1 for an
-// absent page.
+// absent page; `place`: page * page_size + offset, also -1 then.
 struct Slots {
   const KV& kv;
   const int32_t* table;
   uint32_t h;
+  __device__ __forceinline__ int64_t at(uint32_t t, int32_t& place) const {
+    const uint32_t pi = kv.per_page.div(t), page = uint32_t(table[pi]), off = t - pi * kv.page_size;
+    const bool there = page < kv.pages;
+    place = there ? int32_t(page * kv.page_size + off) : -1;
+    return there ? (int64_t(page) * kv.heads + h) * kv.page_size + off : -1;
+  }
   __device__ __forceinline__ int64_t at(uint32_t t) const {
-    const uint32_t pi = kv.per_page.div(t), page = uint32_t(table[pi]);
-    return page < kv.pages ? (int64_t(page) * kv.heads + h) * kv.page_size + (t - pi * kv.page_size) : -1;
+    int32_t place;
+    return at(t, place);
   }
 };
 
@@ -114,16 +120,15 @@ __device__ __forceinline__ void stream_store(uint8_t* p, u32x4 v) {
 
 // Moves first + i, first + i + step, ... of the list, i being the thread's index
 // over 2^lpr_log.
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, int count, const int32_t* table, uint32_t h,
-                                          int lpr_log, int first, int step) {
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, int count, uint32_t h, int lpr_log, int first,
+                                          int step) {
   const int lane = threadIdx.x & ((1 << lpr_log) - 1);
   const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
   for (int i = first + int(threadIdx.x >> lpr_log); i < count; i += step) {
     const int2 move = list[i];
-    const uint32_t tp = a.kv.per_page.div(move.x), fp = a.kv.per_page.div(move.y);
-    const uint32_t tpage = uint32_t(table[tp]), fpage = uint32_t(table[fp]);
-    if (tpage >= a.kv.pages || fpage >= a.kv.pages) continue;
-    const uint32_t toff = move.x - tp * a.kv.page_size, foff = move.y - fp * a.kv.page_size;
+    if (move.x < 0 || move.y < 0) continue;
+    const uint32_t tpage = a.kv.per_page.div(move.x), fpage = a.kv.per_page.div(move.y);
+    const uint32_t toff = move.x - tpage * a.kv.page_size, foff = move.y - fpage * a.kv.page_size;
     const int64_t dst = tpage * a.kv.page_stride + h * a.kv.head_stride + toff * a.kv.slot_stride;
     const int64_t src = fpage * a.kv.page_stride + h * a.kv.head_stride + foff * a.kv.slot_stride;
     if (lane * 16u < bytes) {
@@ -141,8 +146,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, 
   }
 }
 
-// lists: per row the number of moves, the new length, and `most` pairs of a
-// destination and a source.  `alone`: the workgroup moves its rows itself and
+// lists: per row the number of moves, the new length, and `most` pairs of the
+// places of a destination and a source: the mover need not wait for the table.  `alone`: the workgroup moves its rows itself and
 // writes the new length.  Otherwise both are the second kernel's, which is also
 // where lens_out is seq_lens: the workgroups of the other heads still read it
 // here.
@@ -349,8 +354,8 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
       const uint64_t holes = __ballot(hole);
       const uint32_t i = n_moves + (table[k * kWaves + wave] & 0xFFFF) + __popcll(holes & below);
       if (hole) {
-        list[1 + i].x = t;
         if constexpr (KEEP > 0) hole_slot[i] = t;
+        else list[1 + i].x = t;  // until its source is found
       }
     }
     __syncthreads();
@@ -370,10 +375,13 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
         const bool stays = stay_bits >> k & 1, source = t >= keep && stays;
         const uint64_t sources = __ballot(source);
         const uint32_t i = n_sources + (table[k * kWaves + wave] >> 16) + __popcll(sources & below);
-        if (source) list[1 + i].y = t;
-        at[q] = t < n ? slots.at(t) : -1;
+        int2 move = make_int2(-1, -1);
+        at[q] = t < n ? slots.at(t, move.y) : -1;
         to[q] = t < keep && stays && !in_place ? at[q] : -1;
-        if (source) to[q] = slots.at(KEEP ? hole_slot[KEEP ? i : 0] : list[1 + i].x);
+        if (source) {
+          to[q] = slots.at(KEEP ? hole_slot[KEEP ? i : 0] : list[1 + i].x, move.x);
+          list[1 + i] = move;
+        }
         const int64_t of = at[q] >= 0 && to[q] >= 0 ? at[q] : 0;
         w[q] = a.kv.weight[of];
         p[q] = a.kv.position[of];
@@ -398,7 +406,7 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
   if (tid == 0) list[0] = make_int2(int(n_moves), keep);
   if (alone) {
     __syncthreads();
-    move_rows(a, list + 1, int(n_moves), slots.table, slots.h, lpr_log, 0, kSelect >> lpr_log);
+    move_rows(a, list + 1, int(n_moves), slots.h, lpr_log, 0, kSelect >> lpr_log);
   }
 }
 
@@ -410,7 +418,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, const int2
   const int2 head = list[0];
   if (h == 0 && part == 0 && threadIdx.x == 0) a.lens_out[b] = head.y;
   const int per_block = 256 >> lpr_log;
-  move_rows(a, list + 1, head.x, a.seqs.table + b * a.seqs.stride, h, lpr_log, part * per_block, per_row * per_block);
+  move_rows(a, list + 1, head.x, h, lpr_log, part * per_block, per_row * per_block);
 }
 
 // Moves of one row, at most.
