@@ -14,9 +14,11 @@ Quantization for LLM Inference"):
                  significance metric under N:M, then per-vector quantization)
                  and the decomposed product of Section 5.1 in fp64;
 * ``accounting`` the analytic throughput and bits-per-weight counts of
-                 Sections 3.1-3.3 and 5.1.
+                 Sections 3.1-3.3 and 5.1;
+* ``decode``     the operators on the key-value cache (head norms, rotation and
+                 append, attention of one token, eviction) in fp64.
 
 It shares no code with the HIP path.  It is pinned by ``tests/test_oracle_*``
 against closed forms, format definitions, brute force and invariants.
 """
-from . import accounting, formats, sdq  # noqa: F401
+from . import accounting, decode, formats, sdq  # noqa: F401

@@ -25,14 +25,14 @@
 // operand wants, in the key order (g * 4 .. + 3, 16 + g * 4 .. + 3) for lane
 // group g.  Values: a lane loads, for the 8 keys of its group, VPL dimensions
 // (value_dim); pairs of keys are put together with byte permutes, and VPL
-// products follow, one for each dimension of a lane.  The operations are a small
-// part of what the compute units do in the time the cache takes to arrive (170
-// vector instructions and 24 matrix instructions per 16 KiB, 11% of the matrix
-// cores' time and 34% of the vector units' with e4m3), also with one query head
-// in 16 columns, so one kernel serves every head layout.
+// products follow, one for each dimension of a lane.  The operations are a part
+// of what the compute units do in the time the cache takes to arrive (with e4m3,
+// 270 vector and 24 matrix instructions per 8 KiB: vector units 39% busy, matrix
+// cores 12%), also with one query head in 16 columns, so one kernel serves every
+// head layout.
 //
 // What bounds it: the cache's bytes.  A plain streaming read reaches 6.9 TB/s.
-// 64 ragged sequences of up to 8192 e4m3 slots, 32 heads (2.2 GB): 328 us, 6.8
+// 64 ragged sequences of up to 8192 e4m3 slots, 32 heads (2.2 GB): 329 us, 6.7
 // TB/s; one sequence of 131071 slots, 32/8 heads, bf16 (537 MB): 82 us, 6.6, and
 // 4.6 in the second kernel.  Short calls are launches and latency: 100 slots 5.6
 // us, of which 0.9 pass until the lengths are there, 0.6 until the page numbers

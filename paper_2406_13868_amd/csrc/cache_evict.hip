@@ -21,8 +21,9 @@
 //
 // What bounds it: the moved bytes at the rate of a copy where many rows move (32
 // sequences x 32 heads of 8192 slots halved, 2.1 GB read and written: 430 us, 5.0
-// TB/s, beside a selection of 70 that overlaps it, 486 in all); the selection's
-// chain of loads, counts and barriers where few do (641 slots: 7.8 us).
+// TB/s, beside a selection of 70 that overlaps it, 479 in all); the selection's
+// chain of loads, counts and barriers where few do (641 slots: 8 us; 16 x 8 rows
+// of up to 4099 slots 15.7, and 11.3 in the second kernel).
 #include <hip/hip_runtime.h>
 
 #include "kv_cache.h"
