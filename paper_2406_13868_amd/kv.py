@@ -25,14 +25,12 @@ assert _ATTN.size == C.sizeof(_lib.sdq_attn_args)
 assert _EVICT.size == C.sizeof(_lib.sdq_evict_args)
 
 
-def _stream(stream, cache, torch):
-    """The stream to run on: the given one, or the current one of the cache's device."""
-    if stream is not None:
-        return stream.cuda_stream
+def _current_stream(torch, device):
+    """A function that gives the device index's current stream, without a Stream object around it where torch has one."""
     try:
-        return torch._C._cuda_getCurrentRawStream(cache._index)
+        return torch._C._cuda_getCurrentRawStream
     except AttributeError:
-        return torch.cuda.current_stream(cache.device).cuda_stream
+        return lambda _: torch.cuda.current_stream(device).cuda_stream
 
 
 def _ptr(t, shape, dtype, cache, what):
@@ -57,7 +55,7 @@ class KVCache:
     every slot.  The object holds the tensors; it owns no other memory."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "position", "weight", "pages", "heads", "page_size", "dim", "device",
-                 "_c", "_ref", "_index")
+                 "_c", "_ref", "_index", "_current")
 
     def __init__(self, k, v, k_scale=None, v_scale=None, position=None, weight=None):
         torch = _torch()
@@ -85,7 +83,7 @@ class KVCache:
         _same_device(k, v, k_scale, v_scale, position, weight)
         self.k, self.v, self.k_scale, self.v_scale, self.position, self.weight = k, v, k_scale, v_scale, position, weight
         self.pages, self.heads, self.page_size, self.dim = shape
-        self.device, self._index = k.device, k.get_device()
+        self.device, self._index, self._current = k.device, k.get_device(), _current_stream(torch, k.device)
         for t, what in ((k, "k"), (v, "v")):
             if not t.is_cuda:
                 raise ValueError(f"{what} must be a CUDA (HIP) tensor")
@@ -159,7 +157,7 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
         raise ValueError("qkv must be a CUDA (HIP) tensor with contiguous rows")
     if qkv.get_device() != cache._index:
         _same_device(cache.k, qkv)
-    dt = _x_dtype(qkv)
+    dt = _lib.DTYPE_BF16 if qkv.dtype is torch.bfloat16 else _x_dtype(qkv)
     at = _ptr(slot, (M,), torch.int64, cache, "slot")
     where = qw = kw = angles = rot = positions = 0
     if pos is not None:
@@ -181,7 +179,7 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
     rc = (_lib._lib or _lib.lib()).sdq_qkv_append(cache._ref, _APPEND.pack(
         qkv.data_ptr(), where, at, to, qw, kw, angles if rot else 0, M, ld if M > 1 else width, positions, dt,
-        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), _stream(stream, cache, torch))
+        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), stream.cuda_stream if stream is not None else cache._current(cache._index))
     if rc:
         _lib.check(rc, "sdq_qkv_append")
     return out
@@ -213,7 +211,7 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     if not isinstance(q, torch.Tensor) or len(shape := q.shape) != 3 or shape[0] != B or shape[2] != dim:
         raise ValueError(f"q must be [{B}, heads_q, {dim}]")
     heads_q = shape[1]
-    dt = _x_dtype(q)
+    dt = _lib.DTYPE_BF16 if q.dtype is torch.bfloat16 else _x_dtype(q)
     q_ld, head_ld, step = q.stride()
     if not q.is_cuda or step != 1 or (heads_q > 1 and head_ld != dim):
         raise ValueError("q must be a CUDA (HIP) tensor whose sequences are contiguous")
@@ -233,11 +231,12 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
         cap = max_len
     if workspace is None:
         workspace = _workspace(attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), q.device, stream)
-    elif workspace.get_device() != cache._index:
+    elif workspace.get_device() != cache._index or not workspace.is_contiguous():
+        _dev(workspace, "workspace")
         _same_device(cache.k, workspace)
     rc = (_lib._lib or _lib.lib()).sdq_attn_decode(cache._ref, _ATTN.pack(
-        q.data_ptr(), table, lens, to, log, weights, _dev(workspace, "workspace"), workspace.nbytes, B,
-        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), _stream(stream, cache, torch))
+        q.data_ptr(), table, lens, to, log, weights, workspace.data_ptr(), workspace.nbytes, B,
+        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), stream.cuda_stream if stream is not None else cache._current(cache._index))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), "workspace")
@@ -281,11 +280,12 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
         cap = max_len
     if workspace is None:
         workspace = _workspace(cache_evict_workspace_size(cache, B, cap, budget), cache.device, stream)
-    elif workspace.get_device() != cache._index:
+    elif workspace.get_device() != cache._index or not workspace.is_contiguous():
+        _dev(workspace, "workspace")
         _same_device(cache.k, workspace)
     rc = (_lib._lib or _lib.lib()).sdq_cache_evict(cache._ref, _EVICT.pack(
-        table, lens, new, positions, weights, _dev(workspace, "workspace"), workspace.nbytes, B, ld, width, cap, budget, recent),
-        _stream(stream, cache, torch))
+        table, lens, new, positions, weights, workspace.data_ptr(), workspace.nbytes, B, ld, width, cap, budget, recent),
+        stream.cuda_stream if stream is not None else cache._current(cache._index))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, cache_evict_workspace_size(cache, B, cap, budget), "workspace")
