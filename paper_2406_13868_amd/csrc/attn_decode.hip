@@ -90,17 +90,6 @@ __host__ __device__ __forceinline__ int chunks_of(int len, int chunk_log) {
   return n > 1 ? n : 1;
 }
 
-// Inclusive prefix sum over the wave.
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31
-  return v;
-}
-
 // The chunks of the rows of all sequences, sequences in order: `rows` rows each,
 // and `head` units before the chunks of each row.
 // A wave's lanes hold 64 sequences at a time; the first 64 stay in registers.

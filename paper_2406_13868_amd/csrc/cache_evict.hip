@@ -48,11 +48,7 @@ constexpr int kWaves = kSelect / 64;
 // barrier: the scratch (kWaves words) is free again after the next one.
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* waves, uint32_t& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const uint32_t u = __shfl_up(v, k);
-    if (lane >= k) v += u;
-  }
+  v = wave_scan(v);
   if (lane == 63) waves[wave] = v;
   __syncthreads();
   uint32_t before = 0, sum = 0;
@@ -67,9 +63,13 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* waves, uint
 }
 
 __device__ __forceinline__ int block_max(int v, uint32_t* waves) {
-#pragma unroll
-  for (int k = 32; k; k >>= 1) v = max(v, __shfl_xor(v, k));
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = uint32_t(v);
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x111, 0xF, 0xF, false));  // row_shr:1
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x112, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x114, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x142, 0xA, 0xF, false));  // row_bcast:15
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x143, 0xC, 0xF, false));  // row_bcast:31
+  if ((threadIdx.x & 63) == 63) waves[threadIdx.x >> 6] = uint32_t(v);
   __syncthreads();
   int r = int(waves[0]);
 #pragma unroll
