@@ -14,16 +14,18 @@
 // pass in slot order that settles ties and lists what moves by prefix sums.
 // Up to 16384 slots are read once and kept in registers (1, 4, 8 or 16 per thread,
 // the fewest that hold max_len), up to 32768 in shared memory (one sequence of
-// 31853 slots, 4 key heads: 75 us, read again 107); beyond, every pass reads them
-// again from the L2, eight per thread at a time (40000 slots: 142 us).
+// 31853 slots, 4 key heads: 70 us, read again 106); beyond, every pass reads them
+// again from the L2, eight per thread at a time (40000 slots: 129 us).
 // It moves the rows too where that is the faster way; otherwise a second kernel
 // does, 16 bytes per lane.
 //
 // What bounds it: the moved bytes at the rate of a copy where many rows move (32
 // sequences x 32 heads of 8192 slots halved, 2.1 GB read and written: 430 us, 5.0
 // TB/s, beside a selection of 70 that overlaps it, 479 in all); the selection's
-// chain of loads, counts and barriers where few do (641 slots: 8 us; 16 x 8 rows
-// of up to 4099 slots 15.7, and 11.3 in the second kernel).
+// chain of loads, counts and barriers where few do (641 slots: 7 us, of which 1.3
+// until the weights are there, 1.4 for two digits, 0.7 to list the moves, 0.6 to
+// write weights and positions, 2.1 to move rows; 16 x 8 rows of up to 4099 slots
+// 15, and 11 in the second kernel).
 #include <hip/hip_runtime.h>
 
 #include "kv_cache.h"
@@ -440,11 +442,12 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
   const int lpr_log = bytes <= 128 ? 3 : bytes <= 256 ? 4 : 5, per_block = 256 >> lpr_log;
   // Few moves per row cost less than a second launch (16 x 8 rows of 2000 slots, at
-  // most 128 moves: 17.1 us, with one 17.7; 256: 21.0 and 20.7, and the host issues
-  // one launch less; 512: 27.1 and 24.7), and where there are workgroups for two
-  // rounds, some select while others move (32 x 32 rows of 8192 slots, 4096 moves:
-  // 496 us, with a second launch 511).
-  const bool alone = (most <= 256 || rows >= 1024) && a.lens_out != a.seqs.lens;
+  // most 128 moves: 14.1 us, with one 15.0; 256: 16.8 and 17.8; 512: 21.8 and 22.4;
+  // but a single row of 512 moves 14.5 and 11.2, as it is then moved by one
+  // workgroup; 16 x 8 rows of 1000 moves of up to 4099 slots 27.9 and 26.3), and
+  // where there are workgroups for two rounds, some select while others move (32 x
+  // 32 rows of 8192 slots, 4096 moves: 479 us, with a second launch 496).
+  const bool alone = (most <= (rows >= 128 ? 512 : 256) || rows >= 1024) && a.lens_out != a.seqs.lens;
   if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
