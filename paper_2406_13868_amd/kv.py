@@ -179,7 +179,8 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
     rc = (_lib._lib or _lib.lib()).sdq_qkv_append(cache._ref, _APPEND.pack(
         qkv.data_ptr(), where, at, to, qw, kw, angles if rot else 0, M, ld if M > 1 else width, positions, dt,
-        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps), stream.cuda_stream if stream is not None else cache._current(cache._index))
+        dt if out.dtype is qkv.dtype else _x_dtype(out), heads_q, rot, interleaved, eps),
+        stream.cuda_stream if stream is not None else cache._current(cache._index))
     if rc:
         _lib.check(rc, "sdq_qkv_append")
     return out
@@ -236,7 +237,8 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
         _same_device(cache.k, workspace)
     rc = (_lib._lib or _lib.lib()).sdq_attn_decode(cache._ref, _ATTN.pack(
         q.data_ptr(), table, lens, to, log, weights, workspace.data_ptr(), workspace.nbytes, B,
-        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale), stream.cuda_stream if stream is not None else cache._current(cache._index))
+        q_ld if B > 1 else heads_q * dim, ld, width, cap, dt, heads_q, dim ** -0.5 if scale is None else scale),
+        stream.cuda_stream if stream is not None else cache._current(cache._index))
     if rc:
         if rc == _lib.ERR_BUFFER_TOO_SMALL:
             _need_bytes(workspace, attn_decode_workspace_size(cache, B, heads_q, cap, weights != 0), "workspace")
