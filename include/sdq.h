@@ -580,6 +580,9 @@ sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_args* args,
  * they are; the i-th freed slot below it takes the i-th kept slot above it,
  * with its key, value, scales, position and weight.  The order of slots is
  * therefore no longer that of positions, which attention does not need.
+ * Slots on absent pages take no part: they are never kept, and those below the
+ * budget are no places, so that a head keeps as many slots as there are present
+ * ones below the budget.  The new length counts them all the same.
  *   page_table, seq_lens, B, table_stride, max_pages, max_len  as above
  *   lens_out  device, int32 [B]: min(length, budget); may be seq_lens
  *   position_out, weight_out  device, as cache->position and cache->weight:

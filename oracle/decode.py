@@ -60,21 +60,26 @@ def attend(q, k, v, scale) -> Dict[str, np.ndarray]:
                 score_size=(np.abs(q) @ np.abs(k).T * abs(scale)).max(1), out_size=p @ np.abs(v))
 
 
-def evict(weight, position, budget: int, recent: int):
+def evict(weight, position, budget: int, recent: int, present=None):
     """One key head of one sequence: (kept slots that move, ascending; the freed
-    slots they move to, ascending; weight and position afterwards)."""
+    slots they move to, ascending; weight and position afterwards).  Slots that
+    are not present (their page is absent) are no places and are never kept:
+    as many of the others stay as there are present slots below the budget."""
     n = len(weight)
     if n <= budget:
         return np.zeros(0, int), np.zeros(0, int), weight.copy(), position.copy()
-    newest = max(-1, int(position.max()))
-    slots = sorted(range(n), key=lambda t: (not position[t] > newest - recent, math.isnan(weight[t]),
-                                            0.0 if math.isnan(weight[t]) else -float(weight[t]), t))
-    kept = set(slots[:budget])
-    to = np.array([t for t in range(budget) if t not in kept], int)
-    of = np.array([t for t in range(budget, n) if t in kept], int)
+    there = [t for t in range(n) if present is None or present[t]]
+    newest = max([-1] + [int(position[t]) for t in there])
+    slots = sorted(there, key=lambda t: (not position[t] > newest - recent, math.isnan(weight[t]),
+                                         0.0 if math.isnan(weight[t]) else -float(weight[t]), t))
+    places = [t for t in there if t < budget]
+    kept = set(slots[:len(places)])
+    to = np.array([t for t in places if t not in kept], int)
+    of = np.array([t for t in there if t >= budget and t in kept], int)
     w, p = weight.copy(), position.copy()
     w[to], p[to] = weight[of], position[of]
-    w[budget:], p[budget:] = 0, -1
+    given_up = [t for t in there if t >= budget]
+    w[given_up], p[given_up] = 0, -1
     return of, to, w, p
 
 

@@ -4,7 +4,9 @@
 // slots that stay are, in this order: the recent ones (position > newest -
 // recent), then those of the largest weight; equal weights go to the lowest
 // slot.  (If more than the budget are recent, the same order holds among
-// them.)  A NaN weight counts as the lowest.
+// them.)  A NaN weight counts as the lowest.  Slots on absent pages take no part:
+// they are never kept, and those below the budget are no places, so that as many
+// slots stay as there are present ones below the budget.
 // Slots below the budget that stay are not moved.  The i-th freed slot below
 // the budget takes the i-th slot above it that stays, so that the least
 // possible is copied and no copy's source is another's destination.
@@ -36,9 +38,9 @@ namespace {
 constexpr int kSelect = 1024;  // threads of a selecting workgroup
 constexpr int kDigits = 2048;  // values of an 11-bit digit
 
-// Bits that order as the weights do, NaN lowest.
+// Bits that order as the weights do, NaN lowest; 0 is left for absent slots.
 __device__ __forceinline__ uint32_t order_bits(float w) {
-  if (w != w) return 0;
+  if (w != w) return 1;
   w += 0.f;  // -0 and 0 are equal
   const uint32_t u = __float_as_uint(w);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
@@ -186,14 +188,15 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
     return;
   }
 
-  // the thread's slots are k * kSelect + tid; an absent page's have the lowest
-  // weight and are not recent
+  // the thread's slots are k * kSelect + tid; those on absent pages have the key 0
+  // and are not recent
   const int steps = KEEP ? KEEP : (n + kSelect - 1) / kSelect;
   constexpr int kRegs = KEEP ? KEEP : 8;
   constexpr int kNone = INT32_MIN;
   uint32_t keys[kRegs];
   uint32_t recent_bits = 0, recent_all = 0;
-  int edge = kNone;  // a slot is recent if position > edge
+  uint32_t lost = 0;  // of the thread's slots below the budget: those on absent pages
+  int edge = kNone;   // a slot is recent if position > edge
   const auto load = [&](int base, int (&p)[kRegs], bool with_keys) {
 #pragma unroll
     for (int k = 0; k < kRegs; ++k) {
@@ -202,6 +205,7 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
       p[k] = a.kv.position[of];
       if (with_keys) keys[k] = order_bits(a.kv.weight[of]);
       if (at < 0) p[k] = kNone, keys[k] = 0;
+      lost += at < 0 && t < keep;
     }
   };
   const auto set_recent = [&](const int (&p)[kRegs]) {
@@ -230,8 +234,9 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
   };
 
   for (int i = tid; i < 3 * kDigits; i += kSelect) hist[0][i] = 0;
+  if (tid < 9) pick[tid / 3][tid % 3] = 0;  // what it stays where no slot has a place
   int newest = -1;
-  uint32_t recents = 0, total;
+  uint32_t recents = 0, absent, total, all_absent;
   if constexpr (SLOTS == kShared) {
     int p[kShared / kRegs][kRegs];
 #pragma unroll
@@ -251,6 +256,7 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
       recent_all |= recent_bits << (g * kRegs);
     }
     recents = __popc(recent_all);
+    absent = lost;
   } else {
     int p[kRegs];
     for (int base = 0; base < steps; base += kRegs) {
@@ -258,6 +264,7 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
 #pragma unroll
       for (int k = 0; k < kRegs; ++k) newest = max(newest, p[k]);
     }
+    absent = lost;  // later passes load the same slots again
     newest = block_max(newest, waves[0]);
     edge = int(max(int64_t(newest) - a.recent, int64_t(kNone)));
     if constexpr (KEEP > 0) {
@@ -271,10 +278,18 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
       }
     }
   }
-  block_scan(recents, waves[1], total);
-  // the class that is only partly kept, and how many of it
-  const bool among_recent = total >= uint32_t(keep);
-  uint32_t want = among_recent ? keep : keep - total;
+  if constexpr (SLOTS > 0) {  // up to 32768 slots: both counts in one word
+    block_scan(recents | absent << 16, waves[1], total);
+    all_absent = total >> 16;
+    total &= 0xFFFF;
+  } else {
+    block_scan(recents, waves[1], total);
+    block_scan(absent, waves[6], all_absent);
+  }
+  // how many stay, the class that is only partly kept, and how many of it
+  const uint32_t places = uint32_t(keep) - all_absent;
+  const bool among_recent = total >= places;
+  uint32_t want = among_recent ? places : places - total;
 
   // radix selection of the want-th largest weight of that class
   uint32_t prefix = 0, equal = 0;
@@ -311,6 +326,8 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
     equal = pick[pass][2];
   }
 
+  if (places == 0) prefix = ~0u;  // above every key
+
   // in slot order, kRegs steps of the workgroup at a time: what stays, and what moves
   const bool ties = equal > want;
   const uint64_t below = (uint64_t(1) << (tid & 63)) - 1;
@@ -340,6 +357,10 @@ __global__ __launch_bounds__(kSelect, SLOTS && SLOTS <= 8 ? 8 : 4) void evict_se
         if ((eq_bits >> k & 1) && table[k * kWaves + wave] + __popcll(m & below) >= want) stay_bits &= ~(1u << k);
       }
       __syncthreads();
+    }
+    if (all_absent) {  // those below the budget are no holes
+#pragma unroll
+      for (int k = 0; k < kRegs; ++k) stay_bits |= uint32_t(keys[k] == 0 && (base + k) * kSelect + tid < keep) << k;
     }
 #pragma unroll
     for (int k = 0; k < kRegs; ++k) {
