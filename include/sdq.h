@@ -471,10 +471,13 @@ sdq_status sdq_gemm_dual(const sdq_config* cfg, const void* Xq_o, const float* s
  *             of 16 bytes.  Slots do not overlap.
  *   dtype     SDQ_DTYPE_BF16, or SDQ_DTYPE_E4M3: e4m3 codes with one fp32
  *             scale per row (k_scale, v_scale: device, [pages][heads]
- *             [page_size]; NULL otherwise), by sdq_quantize_act's rule with
- *             a row in the place of a token: s = amax / 448, code =
- *             e4m3(x * (448 / amax)), a zero row s = 0 and zero codes.  A row
- *             that holds an infinity or a NaN gets a scale that is not finite.
+ *             [page_size]; NULL otherwise): s = amax / 448, code =
+ *             e4m3(x * (448 / amax)), a zero row s = 0 and zero codes.  That
+ *             is sdq_quantize_act's rule with a row in the place of a token,
+ *             but for two kinds of rows: where 448 / amax would pass fp32's
+ *             range (amax below 1.3e-36) the codes are those of the row times
+ *             2^60, so that it keeps its size; and a row that holds an infinity
+ *             or a NaN gets a scale that is not finite.
  *   position  device, int32 [pages][heads][page_size]: the position of the
  *             token in each slot, or NULL: not kept
  *   weight    device, fp32 [pages][heads][page_size]: the attention weight

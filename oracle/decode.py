@@ -34,13 +34,15 @@ def transform(x, weight, eps, angles, interleaved):
 
 def quantize_row(row32):
     """An fp32 row as e4m3 codes and a scale, by the per-token rule: IEEE fp32
-    operations, nearest even."""
+    operations, nearest even.  A tiny row's codes are those of the row times a
+    power of two, for which 448 / amax is a number."""
     x = np.asarray(row32, np.float32)
     a = np.max(np.abs(x))
     if a == 0:
         return np.zeros(x.shape, np.uint8), np.float32(0)
-    inv = np.float32(448) / a
-    return F.e4m3_encode(x * inv), a / np.float32(448)
+    up = np.float32(2.0 ** 60) if a < 2.0 ** -90 else np.float32(1)
+    inv = np.float32(448) / (a * up)
+    return F.e4m3_encode(x * up * inv), a / np.float32(448)
 
 
 def attend(q, k, v, scale) -> Dict[str, np.ndarray]:

@@ -185,11 +185,14 @@ __global__ __launch_bounds__(256) void qkv_append_kernel(AppendArgs a, FastDiv b
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
 #pragma unroll
     for (int s = LPH / 2; s; s >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), s, LPH)));
-    const float amax = __uint_as_float(top), inv = amax > 0.f ? fminf(448.f / amax, 3.4028235e38f) : 0.f;
+    // 448 / amax is past fp32's range below 1.3e-36: a tiny row is taken times a
+    // power of two, which is exact and does not change the codes of others
+    const float amax = __uint_as_float(top), up = amax < 0x1p-90f ? 0x1p60f : 1.f;
+    const float inv = amax > 0.f ? 448.f / (amax * up) : 0.f;
     if (live) {
       float t[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = fminf(fmaxf(x[i] * inv, -448.f), 448.f);
+      for (int i = 0; i < 8; ++i) t[i] = fminf(fmaxf(x[i] * up * inv, -448.f), 448.f);
       uint32_t lo = 0, hi = 0;
       lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], lo, false);
       lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], lo, true);
