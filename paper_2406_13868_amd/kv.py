@@ -52,7 +52,9 @@ class KVCache:
     elements together and 16-byte aligned, the same for both), k_scale and
     v_scale the fp32 [pages, heads, page_size] scales of e4m3 rows, position
     (int32) and weight (fp32) of the same shape what an evicted cache keeps of
-    every slot.  The object holds the tensors; it owns no other memory."""
+    every slot.  The object holds the tensors; it owns no other memory.  Calls
+    hand their addresses to the library, which are taken here once: none of them
+    can be replaced (with_state() makes a cache with others), what they hold can."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "position", "weight", "pages", "heads", "page_size", "dim", "device",
                  "_c", "_ref", "_index", "_current")
@@ -81,18 +83,31 @@ class KVCache:
             if t is not None:
                 _need(t, shape[:3], dt, what)
         _same_device(k, v, k_scale, v_scale, position, weight)
-        self.k, self.v, self.k_scale, self.v_scale, self.position, self.weight = k, v, k_scale, v_scale, position, weight
-        self.pages, self.heads, self.page_size, self.dim = shape
-        self.device, self._index, self._current = k.device, k.get_device(), _current_stream(torch, k.device)
         for t, what in ((k, "k"), (v, "v")):
             if not t.is_cuda:
                 raise ValueError(f"{what} must be a CUDA (HIP) tensor")
         opt = lambda t, what: None if t is None else _dev(t, what)  # noqa: E731
-        self._c = _lib.sdq_kv_cache(
+        c = _lib.sdq_kv_cache(
             k.data_ptr(), v.data_ptr(), opt(k_scale, "k_scale"), opt(v_scale, "v_scale"), opt(position, "position"),
             opt(weight, "weight"), shape[0], *(0 if n == 1 else s for n, s in zip(shape, stride[:3])),
             _lib.DTYPE_E4M3 if e4m3 else _lib.DTYPE_BF16, *shape[1:])
-        self._ref = C.byref(self._c)
+        for name, value in zip(KVCache.__slots__, (k, v, k_scale, v_scale, position, weight, *shape, k.device, c, C.byref(c),
+                                                   k.get_device(), _current_stream(torch, k.device))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        if name in KVCache.__slots__:
+            raise AttributeError(f"{name} of a cache is fixed: its address or size is the library's already; with_state() makes a "
+                                 "cache with other positions and weights, KVCache() one with other tensors")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in KVCache.__slots__:
+            raise AttributeError(f"{name} of a cache is fixed: with_state() or KVCache() makes another cache")
+        object.__delattr__(self, name)
+
+    def __reduce__(self):  # a copy takes the addresses of its own tensors
+        return type(self), (self.k, self.v, self.k_scale, self.v_scale, self.position, self.weight)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, dim: int, dtype: str = "bf16", track: bool = False,
