@@ -106,6 +106,7 @@ extern "C" sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_append
   if (M == 0) return SDQ_OK;
   if (!t->qkv || !t->slot || !t->q_out || (t->rot_dim && !t->cos_sin) || ((t->rot_dim || cache->position) && !t->pos))
     return SDQ_ERR_NULL;
+  if (t->rot_dim && t->positions == 0) return SDQ_ERR_SHAPE;  // the kernel reads row 0 for a position outside the table
   if (!aligned16(t->qkv) || !aligned16(t->q_out) || !aligned16(t->q_weight) || !aligned16(t->k_weight) ||
       !aligned16(t->cos_sin))
     return SDQ_ERR_SHAPE;
