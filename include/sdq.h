@@ -513,8 +513,8 @@ typedef struct {
  *   q_weight, k_weight  device, fp32 [dim], 16-byte aligned, both or neither:
  *            every query (key) head becomes x * weight / sqrt(mean x^2 + eps)
  *   cos_sin  device, fp32 [positions][rot_dim], 16-byte aligned: for each
- *            position the rot_dim / 2 cosines, then the sines; NULL with
- *            rot_dim = 0
+ *            position the rot_dim / 2 cosines, then the sines, of at least
+ *            one position; NULL with rot_dim = 0
  *   rot_dim  leading dimensions of a head that are rotated: even, 0 to dim
  *   interleaved  0: dimension i is paired with i + rot_dim / 2; 1: 2i with 2i + 1.
  *            A pair (a, b) becomes (a cos - b sin, b cos + a sin).
