@@ -11,6 +11,10 @@ fallback: if the library is missing every call raises.
     packed = torch.from_numpy(blob).cuda()
     Xq, s_a = quantize_act(X_cuda, cfg)      # per-token activation quantization
     Y = gemm(Xq, s_a, packed, N, K, cfg)     # Y = s_a * Xq (W_o + W_i)^T (Section 5.1)
+
+Calls with `stream` run there, not on the current stream, and do not wait for it:
+the caller orders them after what makes their arguments, and what they return
+before its use elsewhere (wait_stream).
 """
 from __future__ import annotations
 
@@ -321,21 +325,35 @@ def _same_device(first, *ts):
             raise ValueError(f"tensors are on different devices: {sorted(map(str, devs))}")
 
 
-def _workspace(nbytes: int, device, stream):
-    """A fresh workspace of one call: kept from reuse until the stream that the
-    call runs on is done with it, where that is not the current one."""
+def _empty(shape, dtype, device, stream, returned: bool = True):
+    """A fresh tensor of one call, from the memory of the stream that the call
+    runs on.  From the current stream's it could be a block that was freed while
+    work queued there still reads it, and another stream would not wait for that.
+    Where it is returned, its memory's next use waits for what the current stream
+    has queued by the time it is freed."""
     torch = _torch()
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
-    return ws
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if stream.cuda_stream == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(current)
+    return t
 
 
-def _out(out, M: int, N: int, cfg: Config, device):
+def _workspace(nbytes: int, device, stream):
+    """A fresh workspace of one call."""
+    return _empty(nbytes, _torch().uint8, device, stream, returned=False)
+
+
+def _out(out, M: int, N: int, cfg: Config, device, stream):
     """The GEMM output: `out` checked against [M, N] of cfg's output dtype, or a new tensor."""
     dt = cfg.y_torch_dtype()
     if out is None:
-        return _torch().empty((M, N), dtype=dt, device=device)
+        return _empty((M, N), dt, device, stream)
     if out.shape != (M, N) or out.dtype != dt:
         raise ValueError(f"out must be [{M}, {N}] {dt}, got {list(out.shape)} {out.dtype}")
     return out
@@ -348,8 +366,8 @@ def quantize_act(X, cfg: Config, out=None, scales=None, stream=None):
         raise ValueError("X must be [M, K]")
     M, K = X.shape
     dt = _x_dtype(X)
-    Xq = out if out is not None else torch.empty((M, K), dtype=torch.uint8, device=X.device)
-    s_a = scales if scales is not None else torch.empty((M,), dtype=torch.float32, device=X.device)
+    Xq = out if out is not None else _empty((M, K), torch.uint8, X.device, stream)
+    s_a = scales if scales is not None else _empty((M,), torch.float32, X.device, stream)
     _need(Xq, (M, K), torch.uint8, "Xq")
     _need(s_a, (M,), torch.float32, "s_a")
     _same_device(X, Xq, s_a)
@@ -372,10 +390,10 @@ def quantize_act_dual(X, cfg: Config, out=None, stream=None):
     if out is not None:
         Xo, s_a, Xi, Ea = out
     else:
-        Xo = torch.empty((M, K), dtype=torch.uint8, device=dev)
-        s_a = torch.empty((M,), dtype=torch.float32, device=dev)
-        Xi = torch.empty((M, K // 2), dtype=torch.uint8, device=dev)
-        Ea = torch.empty((M, K // 32), dtype=torch.uint8, device=dev)
+        Xo = _empty((M, K), torch.uint8, dev, stream)
+        s_a = _empty((M,), torch.float32, dev, stream)
+        Xi = _empty((M, K // 2), torch.uint8, dev, stream)
+        Ea = _empty((M, K // 32), torch.uint8, dev, stream)
     _need(Xo, (M, K), torch.uint8, "Xq_o")
     _need(s_a, (M,), torch.float32, "s_a_o")
     _need(Xi, (M, K // 2), torch.uint8, "Xq_i")
@@ -398,7 +416,7 @@ def gemm_dual(Xo, s_a, Xi, Ea, packed, N: int, K: int, cfg: Config, out=None, st
     _need(Xi, (M, K // 2), torch.uint8, "Xq_i")
     _need(Ea, (M, K // 32), torch.uint8, "e_a_i")
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
-    Y = _out(out, M, N, cfg, Xo.device)
+    Y = _out(out, M, N, cfg, Xo.device, stream)
     _same_device(Xo, s_a, Xi, Ea, packed, Y)
     _lib.check(_lib.lib().sdq_gemm_dual(cfg._ref, _dev(Xo, "Xq_o"), _dev(s_a, "s_a_o"),
                                         _dev(Xi, "Xq_i"), _dev(Ea, "e_a_i"), M, _dev(packed, "packed"),
@@ -429,7 +447,7 @@ def gemm(Xq, s_a, packed, N: int, K: int, cfg: Config, out=None, path: int = PAT
     _need(Xq, (M, K), torch.uint8, "Xq")
     _need(s_a, (M,), torch.float32, "s_a")
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
-    Y = _out(out, M, N, cfg, Xq.device)
+    Y = _out(out, M, N, cfg, Xq.device, stream)
     _same_device(Xq, s_a, packed, Y, workspace)
     ws_bytes = gemm_workspace_size(cfg, M, N, K, path)
     if ws_bytes == 0 and path not in (PATH_DENSE, PATH_SPLITK):
@@ -454,7 +472,7 @@ def unpack_weights(packed, N: int, K: int, cfg: Config, workspace=None, stream=N
     torch = _torch()
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
     nb = gemm_workspace_size(cfg, 0, N, K, PATH_DENSE)
-    ws = workspace if workspace is not None else torch.empty(nb, dtype=torch.uint8, device=packed.device)
+    ws = workspace if workspace is not None else _empty(nb, torch.uint8, packed.device, stream)
     _need_bytes(ws, nb, "workspace")
     _same_device(packed, ws)
     _lib.check(_lib.lib().sdq_unpack_weights(cfg._ref, _dev(packed, "packed"), N, K,
@@ -475,7 +493,7 @@ def gemm_unpacked(Xq, s_a, packed, N: int, K: int, cfg: Config, workspace, out=N
     _need(s_a, (M,), torch.float32, "s_a")
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
     _need_bytes(workspace, gemm_workspace_size(cfg, M, N, K, PATH_DENSE), "workspace")
-    Y = _out(out, M, N, cfg, Xq.device)
+    Y = _out(out, M, N, cfg, Xq.device, stream)
     _same_device(Xq, s_a, packed, Y, workspace)
     _lib.check(_lib.lib().sdq_gemm_unpacked(cfg._ref, _dev(Xq, "Xq"), _dev(s_a, "s_a"), M,
                                             _dev(packed, "packed"), N, K, _dev(workspace, "workspace"),
@@ -495,7 +513,7 @@ def gemm_static(Xq, s_a, packed, N: int, K: int, cfg: Config, out=None, path: in
     _need(Xq, (M, K), torch.uint8, "Xq")
     _need(s_a, (M,), torch.float32, "s_a")
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
-    Y = _out(out, M, N, cfg, Xq.device)
+    Y = _out(out, M, N, cfg, Xq.device, stream)
     _same_device(Xq, s_a, packed, Y)
     _lib.check(_lib.lib().sdq_gemm_static(cfg._ref, _dev(Xq, "Xq"), _dev(s_a, "s_a"), M,
                                           _dev(packed, "packed"), N, K, _dev(Y, "Y"),
@@ -514,12 +532,12 @@ def linear(X, packed, N: int, K: int, cfg: Config, out=None, xq=None, scales=Non
         raise ValueError(f"X must be [M, {K}], got {list(X.shape)}")
     M = X.shape[0]
     dt = _x_dtype(X)
-    Xq = xq if xq is not None else torch.empty((M, K), dtype=torch.uint8, device=X.device)
-    s_a = scales if scales is not None else torch.empty((M,), dtype=torch.float32, device=X.device)
+    Xq = xq if xq is not None else _empty((M, K), torch.uint8, X.device, stream)
+    s_a = scales if scales is not None else _empty((M,), torch.float32, X.device, stream)
     _need(Xq, (M, K), torch.uint8, "Xq")
     _need(s_a, (M,), torch.float32, "s_a")
     _need_bytes(packed, pack_size(cfg, N, K), "packed")
-    Y = _out(out, M, N, cfg, X.device)
+    Y = _out(out, M, N, cfg, X.device, stream)
     _same_device(X, Xq, s_a, packed, Y, workspace)
     args = (cfg._ref, _dev(X, "X"), dt, M, _dev(Xq, "Xq"), _dev(s_a, "s_a"), _dev(packed, "packed"), N, K,
             _dev(Y, "Y"))

@@ -13,7 +13,7 @@ from __future__ import annotations
 import ctypes as C
 import struct
 
-from . import _dev, _lib, _need, _need_bytes, _same_device, _torch, _workspace, _x_dtype
+from . import _dev, _empty, _lib, _need, _need_bytes, _same_device, _torch, _workspace, _x_dtype
 
 # The argument structures as bytes: packing one takes a fraction of the time
 # that filling a ctypes structure, or passing as many arguments, does.
@@ -190,7 +190,7 @@ def qkv_append(qkv, pos, slot, cache: KVCache, heads_q: int, cos_sin=None, inter
     elif q_weight is not None or k_weight is not None:
         raise ValueError("q_weight and k_weight go together")
     if out is None:
-        out = torch.empty((M, heads_q, dim), dtype=out_dtype or qkv.dtype, device=qkv.device)
+        out = _empty((M, heads_q, dim), out_dtype or qkv.dtype, qkv.device, stream)
     to = _ptr(out, (M, heads_q, dim), out_dtype or out.dtype, cache, "out")
     rc = (_lib._lib or _lib.lib()).sdq_qkv_append(cache._ref, _APPEND.pack(
         qkv.data_ptr(), where, at, to, qw, kw, angles if rot else 0, M, ld if M > 1 else width, positions, dt,
@@ -234,7 +234,7 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
     if q.get_device() != cache._index:
         _same_device(cache.k, q)
     if out is None:
-        out = torch.empty((B, heads_q, dim), dtype=q.dtype, device=q.device)
+        out = _empty((B, heads_q, dim), q.dtype, q.device, stream)
     to = _ptr(out, shape, q.dtype, cache, "out")
     log = 0 if lse is None else _ptr(lse, (B, heads_q), torch.float32, cache, "lse")
     weights = 0
@@ -290,7 +290,7 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
     weights = _ptr(weight_out, shape, torch.float32, cache, "weight_out")
     positions = _ptr(position_out, shape, torch.int32, cache, "position_out")
     if lens_out is None:
-        lens_out = torch.empty_like(seq_lens)
+        lens_out = _empty((B,), seq_lens.dtype, cache.device, stream)
     new = _ptr(lens_out, (B,), torch.int32, cache, "lens_out")
     cap = width * cache.page_size
     if max_len is not None and max_len < cap:
