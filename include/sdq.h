@@ -587,7 +587,7 @@ sdq_status sdq_attn_decode(const sdq_kv_cache* cache, const sdq_attn_args* args,
  * budget are no places, so that a head keeps as many slots as there are present
  * ones below the budget.  The new length counts them all the same.
  *   page_table, seq_lens, B, table_stride, max_pages, max_len  as above
- *   lens_out  device, int32 [B]: min(length, budget); may be seq_lens
+ *   lens_out  device, int32 [B]: min(length, budget); may be or overlap seq_lens
  *   position_out, weight_out  device, as cache->position and cache->weight:
  *             either both those very pointers, or both apart from them.  Slots
  *             below the new length get the kept slots' values, those from there

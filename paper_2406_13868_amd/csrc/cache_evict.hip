@@ -154,8 +154,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const int2* list, 
 // lists: per row the number of moves, the new length, and `most` pairs of the
 // places of a destination and a source: the mover need not wait for the table.  `alone`: the workgroup moves its rows itself and
 // writes the new length.  Otherwise both are the second kernel's, which is also
-// where lens_out is seq_lens: the workgroups of the other heads still read it
-// here.
+// where lens_out overlaps seq_lens: other workgroups still read it here.
 // KEEP: slots per thread kept in registers, up to 8 of which leave room for two
 // workgroups on a compute unit.  kShared: 32 of them, the keys in shared memory
 // (in registers they spill).  0: read again in every pass.
@@ -468,7 +467,9 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   // workgroup; 16 x 8 rows of 1000 moves of up to 4099 slots 27.9 and 26.3), and
   // where there are workgroups for two rounds, some select while others move (32 x
   // 32 rows of 8192 slots, 4096 moves: 479 us, with a second launch 496).
-  const bool alone = (most <= (rows >= 128 ? 512 : 256) || rows >= 1024) && a.lens_out != a.seqs.lens;
+  // It writes lens_out while other workgroups read seq_lens: not where they overlap.
+  const bool apart = a.lens_out + a.seqs.B <= a.seqs.lens || a.seqs.lens + a.seqs.B <= a.lens_out;
+  const bool alone = (most <= (rows >= 128 ? 512 : 256) || rows >= 1024) && apart;
   if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
