@@ -237,76 +237,66 @@ __device__ __forceinline__ void head_stats(const AttnArgs& a, const Plan& p, con
   for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
 }
 
-// Outputs of query heads qh0 .. qh0 + heads - 1 (heads h0 .. of their row) from the
-// parts of the row, by the whole workgroup.  dim / 4 threads per head and set of
-// parts; each set joins its own as they arrive, four requested at a time, and the
-// sets meet in shared memory (sm: 1024 floats, sm_ml: 128).
+// Output of query head qh (head h of its row) from the parts of the row, by the
+// whole workgroup.  dim / 4 threads per set of parts; each set joins its own as
+// they arrive, four requested at a time, and the sets meet in shared memory (sm:
+// 1024 floats, sm_ml: 128).
 template <bool F32>
-__device__ __forceinline__ void join_heads(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp, int64_t qh0,
-                                           int h0, int heads, float* sm, float* sm_ml) {
+__device__ __forceinline__ void join_head(const AttnArgs& a, const Plan& p, const Ranges& ranges, const RowParts& rp, int64_t qh, int h,
+                                          float* sm, float* sm_ml) {
   const uint32_t D = a.kv.dim;
-  const int per = int(D) / 4, groups = 256 / per, group = threadIdx.x / per, d = (threadIdx.x - group * per) * 4;
-  for (int base = 0; base < heads; base += groups) {
-    const int n = min(heads - base, groups), sets = groups / n, h = group % n, set = group / n;
-    const bool mine = group < n * sets;
-    float top = kNegInf, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (mine)
-      for (int w = rp.w0 + set; w <= rp.w1; w += 4 * sets) {
-        float pm[4], pl[4];
-        float4 po[4];
+  const int per = int(D) / 4, sets = 256 / per, set = threadIdx.x / per, d = (threadIdx.x - set * per) * 4;
+  const bool mine = set < sets;
+  float top = kNegInf, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
+  if (mine)
+    for (int w = rp.w0 + set; w <= rp.w1; w += 4 * sets) {
+      float pm[4], pl[4];
+      float4 po[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const bool in = w + k * sets <= rp.w1;
-          const float* part = rp.part(p, ranges, in ? w + k * sets : w);
-          pm[k] = in ? part[p.gh * D + h0 + base + h] : kNegInf;
-          pl[k] = part[p.gh * D + p.gh + h0 + base + h];
-          po[k] = *reinterpret_cast<const float4*>(part + (h0 + base + h) * D + d);
-        }
-        const float t = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), top), ref = t == kNegInf ? 0.f : t;
-        const float old = __builtin_amdgcn_exp2f(top - ref);
-        sum *= old;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) r[x] *= old;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
-          sum += f * pl[k];
-          r[0] += f * po[k].x;
-          r[1] += f * po[k].y;
-          r[2] += f * po[k].z;
-          r[3] += f * po[k].w;
-        }
-        top = t;
+      for (int k = 0; k < 4; ++k) {
+        const bool in = w + k * sets <= rp.w1;
+        const float* part = rp.part(p, ranges, in ? w + k * sets : w);
+        pm[k] = in ? part[p.gh * D + h] : kNegInf;
+        pl[k] = part[p.gh * D + p.gh + h];
+        po[k] = *reinterpret_cast<const float4*>(part + h * D + d);
       }
-    __syncthreads();  // what the shared memory held has been read
-    *reinterpret_cast<float4*>(&sm[threadIdx.x * 4]) = make_float4(r[0], r[1], r[2], r[3]);
-    if (d == 0 && mine) {
-      sm_ml[group] = top;
-      sm_ml[64 + group] = sum;
+      const float t = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), top), ref = t == kNegInf ? 0.f : t;
+      const float old = __builtin_amdgcn_exp2f(top - ref);
+      sum *= old;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) r[x] *= old;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(pm[k] - ref);
+        sum += f * pl[k];
+        r[0] += f * po[k].x;
+        r[1] += f * po[k].y;
+        r[2] += f * po[k].z;
+        r[3] += f * po[k].w;
+      }
+      top = t;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n * int(D); i += 256) {
-      const int hh = i / int(D), x = i - hh * int(D);
-      float most = kNegInf;
-      for (int k = 0; k < sets; ++k) most = fmaxf(most, sm_ml[k * n + hh]);
-      const float ref = most == kNegInf ? 0.f : most;
-      float total = 0.f, y = 0.f;
-      for (int k = 0; k < sets; ++k) {
-        const float f = __builtin_amdgcn_exp2f(sm_ml[k * n + hh] - ref);
-        total += f * sm_ml[64 + k * n + hh];
-        y += f * sm[(k * n + hh) * int(D) + x];
-      }
-      const int64_t qh = qh0 + base + hh;
-      y *= total == 0.f ? 0.f : 1.f / total;
-      if constexpr (F32) static_cast<float*>(a.out)[qh * D + x] = y;
-      else static_cast<__bf16*>(a.out)[qh * D + x] = static_cast<__bf16>(y);
-      if (x == 0) {
-        const float lse2 = most + __log2f(total);
-        p.lse2[qh] = lse2;
-        if (a.lse) a.lse[qh] = lse2 * kLn2;
-      }
-    }
+  *reinterpret_cast<float4*>(&sm[threadIdx.x * 4]) = make_float4(r[0], r[1], r[2], r[3]);
+  if (d == 0 && mine) {
+    sm_ml[set] = top;
+    sm_ml[64 + set] = sum;
   }
+  __syncthreads();
+  const int x = threadIdx.x;
+  if (x >= int(D)) return;
+  float most = kNegInf;
+  for (int k = 0; k < sets; ++k) most = fmaxf(most, sm_ml[k]);
+  const float ref = most == kNegInf ? 0.f : most;
+  float total = 0.f, y = 0.f;
+  for (int k = 0; k < sets; ++k) {
+    const float f = __builtin_amdgcn_exp2f(sm_ml[k] - ref);
+    total += f * sm_ml[64 + k];
+    y += f * sm[k * int(D) + x];
+  }
+  y *= total == 0.f ? 0.f : 1.f / total;
+  if constexpr (F32) static_cast<float*>(a.out)[qh * D + x] = y;
+  else static_cast<__bf16*>(a.out)[qh * D + x] = static_cast<__bf16>(y);
+  if (x == 0 && a.lse) a.lse[qh] = (most + __log2f(total)) * kLn2;
 }
 
 // The dimension of value product j in row c: VPL = DP / 16 neighbouring ones per
@@ -792,7 +782,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan p, int 
     const int h = hq - hk * int(a.group) - gi * 16;
     const RowParts rp = RowParts::of(all, ranges, b, hk * int(p.hgroups) + gi);
     if (rp.w0 == rp.w1) return;  // the row was finished in one workgroup
-    join_heads<F32>(a, p, ranges, rp, int64_t(b) * a.heads_q + hq, h, 1, sm, sm_ml);
+    join_head<F32>(a, p, ranges, rp, int64_t(b) * a.heads_q + hq, h, sm, sm_ml);
     return;
   }
   id -= joins;
