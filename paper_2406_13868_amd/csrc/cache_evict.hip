@@ -461,15 +461,23 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const int most = int(most_moves(a.seqs.cap, a.budget)), rows = a.seqs.B * int(a.kv.heads);
   const uint32_t bytes = a.kv.dim * (a.kv.e4m3 ? 1 : 2);
   const int lpr_log = bytes <= 128 ? 3 : bytes <= 256 ? 4 : 5, per_block = 256 >> lpr_log;
-  // Few moves per row cost less than a second launch (16 x 8 rows of 2000 slots, at
-  // most 128 moves: 14.1 us, with one 15.0; 256: 16.8 and 17.8; 512: 21.8 and 22.4;
-  // but a single row of 512 moves 14.5 and 11.2, as it is then moved by one
-  // workgroup; 16 x 8 rows of 1000 moves of up to 4099 slots 27.9 and 26.3), and
-  // where there are workgroups for two rounds, some select while others move (32 x
-  // 32 rows of 8192 slots, 4096 moves: 479 us, with a second launch 496).
+  // The selecting workgroup moves its own rows where few do, which costs less than
+  // a second launch (us, with one in brackets; dim 128, bf16): at most 256 moves,
+  // 1 row 8.2 (8.6), 64 rows 10.7 (11.4), 256 rows 16.6 (19.3); of 384 moves 1 row
+  // 11.6 (11.0), 64 rows 16.3 (15.4), 112 rows 18.2 (18.2), 128 rows 18.4 (18.5), 160
+  // rows 19.4 (21.4); of 512 moves 96 rows 21.2 (19.4), 128 rows 22.2 (21.9), 160 rows
+  // 24.0 (24.0), 192 rows 25.4 (27.4).
+  // With more moves it is a matter of the rows alone: 128 keep half of the compute
+  // units, 192 and more enough of them, and some rows are selected while others
+  // move.  Up to 4000 slots, 2000 moves: 128 rows 41.4 (40.1), 160 rows
+  // 46.0 (47.7), 192 rows 52.1 (54.6), 256 rows 66.3 (69.0); 8000 slots, 4000 moves:
+  // 78.0 (73.8), 87.3 (87.8), 99.8 (102.8), 130 (133), and 1024 rows 490 (507); 16000
+  // slots, 8000 moves: 153 (144), 173 (171), 196 (201), 250 (256); 24000 slots, dim 64,
+  // 256 rows 227 (229).  e4m3, 8000 slots: 160 rows 62.0 (58.5), 192 rows 66.0 (66.0),
+  // 224 rows 70.5 (74.3).
   // It writes lens_out while other workgroups read seq_lens: not where they overlap.
   const bool apart = a.lens_out + a.seqs.B <= a.seqs.lens || a.seqs.lens + a.seqs.B <= a.lens_out;
-  const bool alone = (most <= (rows >= 128 ? 512 : 256) || rows >= 1024) && apart;
+  const bool alone = (most <= (rows >= 128 ? 512 : 256) || rows >= 192) && apart;
   if (a.seqs.cap <= kSelect) evict_select_kernel<1><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 4 * kSelect) evict_select_kernel<4><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);
   else if (a.seqs.cap <= 8 * kSelect) evict_select_kernel<8><<<rows, kSelect, 0, st>>>(a, ws, most, alone, lpr_log);

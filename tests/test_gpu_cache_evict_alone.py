@@ -17,6 +17,7 @@ CASES = [
     ([33000], 2, 16, 128, "e4m3", 32800, 500),
     ([300, 800], 64, 16, 16, "bf16", 290, 20),   # 128 rows of up to 510 moves
     ([90] * 31 + [700], 32, 16, 32, "e4m3", 60, 9),  # 1024 rows
+    ([2000, 1700] * 12, 8, 16, 64, "bf16", 900, 30),  # 192 rows, of up to 900 moves
     ([1500] + [70] * 7, 128, 16, 48, "bf16", 700, 9),  # 1024 rows, of up to 700 moves
 ]
 
