@@ -908,8 +908,15 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool f32, hipStream_t st) {
   // bytes per slot), the second kernel 4 (one sequence of 512 slots, 32 heads of
   // 128, bf16: 10.0 us, split 10.3; of 256 7.4 and 9.5; of 700 not split 11.9, 10.7;
   // 8 heads of 256, 256 slots 10.3 and 11.7, 400 not split 12.7, 11.6).  Nor are
-  // somewhat longer ones where they fill the GPU as they are (32 sequences of 800
-  // e4m3 slots, 8 key heads: 15.1, split 20.8).
+  // somewhat longer ones where they fill the GPU as they are.  Rows of 1000 slots,
+  // heads of 128, e4m3 (us, split in brackets): 64 rows 14.7 (12.4), 128 rows 15.1
+  // (14.9), 192 rows 15.4 (18.2), 256 rows 16.1 (20.7), 300 rows 22.4 (25.8), 512 rows
+  // 25.3 (29.0); and of 1300 slots 128 rows 18.3 (16.8), 320 rows 27.2 (28.9).  With
+  // lengths spread evenly below 1000 it takes more rows, which the host cannot know:
+  // 128 rows 20.7 (13.7), 240 rows 17.4 (16.5), 256 rows 18.8 (17.6), 512 rows 23.9
+  // (25.6), 2048 rows 60.6 (73.7).  Rows of 512 bytes per slot, one workgroup to a
+  // compute unit: 256 rows of 1000 43.1 (44.8), 300 rows 66.5 (56.0), 512 rows 83.7
+  // (86.4).
   p.whole = most <= (row_bytes > 256 ? 2 : 4) || (rows >= kMostGroups / 2 && most <= 8);
   // The first loads' latency and the join of the waves take the time of about
   // two chunks; counted, workgroups with many short rows are not the last to
@@ -928,10 +935,12 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool f32, hipStream_t st) {
   groups = std::min(groups, p.whole ? rows : rows * (p.head + most));
   p.groups = uint32_t(groups);
   // A whole row's workgroup adds its attention weights itself: no second launch
-  // (one sequence of 300 slots, 32 heads 9.8 us, with one 12.1; 64 of 128 32.2
-  // and 36.6; 32 of 800 e4m3 slots, 8 key heads 19.3 and 21.3; 128 of up to 1000
-  // 68.5 and 67.5).  Where a key head's query heads are several rows, the second
-  // kernel sums over them.
+  // (one sequence of 300 slots, 32 heads 9.4 us, with one 12.1; 32 of 100 16.1 and
+  // 20.0, of 500 46.9 and 48.1; 64 of 500, 8 key heads, 23.4 and 26.7).  It is as
+  // fast where many query heads share 1000 slots (128 sequences of 1000 e4m3 slots,
+  // 32/8 heads: 67.3 and 65.9; of bf16, 8 heads, 91.9 and 91.9), which is not told
+  // apart.  Where a key head's query heads are several rows, the second kernel sums
+  // over them.
   p.weigh = track && p.whole && s.hgroups == 1;
   p.score_ld = s.score_ld;
   p.part = a.ws;
