@@ -553,7 +553,9 @@ sdq_status sdq_qkv_append(const sdq_kv_cache* cache, const sdq_append_args* args
  *             sdq_attn_decode_workspace_size(cache, B, heads_q, max_len, track) bytes,
  *             max_len as given here or min(max_len, max_pages * page_size), track:
  *             weight_out is not NULL.  Scratch, as in sdq_gemm_ws.
- * A sequence without a slot gives zeros and lse = -inf.  Scores, softmax and
+ * A sequence without a slot gives zeros and lse = -inf.  A NaN in a live slot
+ * reaches the query heads that read it; an infinity in a live key, value or scale
+ * reaches them as such or as a NaN.  Scores, softmax and
  * sums are fp32; the probabilities enter the second product with 17 bits (bf16
  * outputs) or 24 (fp32).  Deterministic.  B = 0 is a no-op; B up to 2^20, with
  * B * heads * ceil(heads_q / heads / 16) * (ceil(max_len / 128) + 8) below

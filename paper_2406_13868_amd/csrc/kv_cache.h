@@ -8,7 +8,9 @@
 
 namespace sdq {
 
-// n / d for 0 <= n < 2^31 by a multiplication: with l = ceil(log2 d) and
+// n / d for 0 <= n < 2^31 by a multiplication with a reciprocal that is rounded up
+// (Granlund and Montgomery, "Division by Invariant Integers using Multiplication",
+// 1994): with l = ceil(log2 d) and
 // m = floor(2^32 (2^l - d) / d) + 1, n / d = (umulhi(m, n) + n) >> l.
 struct FastDiv {
   uint32_t d, m, l;

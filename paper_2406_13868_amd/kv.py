@@ -5,8 +5,8 @@ marshalled here and all work is done by the library's kernels.
 
     cache = KVCache.empty(pages, heads, page_size, dim, "e4m3", track=True)
     q = qkv_append(qkv, pos, slot, cache, heads_q, cos_sin)       # norm, rotation, append
-    o = attn_decode(q, cache, page_table, seq_lens, weight_out=cache.weight)
-    seq_lens = cache_evict(cache, page_table, seq_lens, budget=4096, recent=256)
+    o = attn_decode(q, cache, page_table, seq_lens, max_len=longest, weight_out=cache.weight)
+    seq_lens = cache_evict(cache, page_table, seq_lens, budget=4096, recent=256, max_len=longest)
 """
 from __future__ import annotations
 
@@ -215,7 +215,10 @@ def attn_decode(q, cache: KVCache, page_table, seq_lens, max_len=None, scale=Non
 
     q is [B, heads_q, dim], fp32 or bf16 (sequences may be strided), page_table
     int32 [B, pages], seq_lens int32 [B]; max_len is an upper bound of the
-    lengths (default: what the page table holds), scale defaults to dim ** -0.5.
+    lengths (default: what the page table holds).  It should be given where the
+    table has room for far longer sequences: it sizes the launches and the
+    workspace (with weight_out 4 bytes per query head and slot of max_len) and
+    picks the kernels' form.  scale defaults to dim ** -0.5.
     lse (fp32 [B, heads_q]) receives the logarithm of the softmax sums.
     weight_out (cache.weight itself, or a tensor like it) receives cache.weight
     plus each slot's attention weight, summed over the query heads of its key
@@ -273,7 +276,7 @@ def cache_evict(cache: KVCache, page_table, seq_lens, budget: int, recent: int =
                 weight_out=None, position_out=None, workspace=None, stream=None):
     """Keep `budget` slots of every longer sequence, per key head: the recent
     ones, then those of the largest weight.  Returns the new lengths, in lens_out
-    (which may be seq_lens) or a new tensor.
+    (which may be seq_lens) or a new tensor.  max_len: as in attn_decode.
 
     Keys, values and scales move in place.  Positions and weights are updated in
     place too, or written to position_out and weight_out (both, and not the
