@@ -23,8 +23,8 @@
 //
 // What bounds it: the moved bytes at the rate of a copy where many rows move (32
 // sequences x 32 heads of 8192 slots halved, 2.1 GB read and written: 430 us, 5.0
-// TB/s, beside a selection of 70 that overlaps it, 479 in all); the selection's
-// chain of loads, counts and barriers where few do (641 slots: 7 us, of which 1.3
+// TB/s, beside a selection of 70 that overlaps it, 485 in all); the selection's
+// chain of loads, counts and barriers where few do (641 slots: 7.6 us, of which 1.3
 // until the weights are there, 1.4 for two digits, 0.7 to list the moves, 0.6 to
 // write weights and positions, 2.1 to move rows; 16 x 8 rows of up to 4099 slots
 // 15, and 11 in the second kernel).
