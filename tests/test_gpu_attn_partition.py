@@ -111,3 +111,34 @@ def test_every_slot_counts_once(case, track):
         tol = (2 * math.log2(max(lens) + 1) + 4 + g) * U
         live = live[:, None, :].repeat(heads, 1)
         assert np.all(np.abs(w - want)[live] <= tol * want[live]) and np.all(w[~live] == -3)
+
+
+@pytest.mark.parametrize("lens", [[300, 5], [3000, 1, 0, 2047]], ids=str)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scales_that_are_aligned_to_their_type_only(lens, dim):
+    """e4m3 scales four bytes past a 16-byte boundary: another path to the same exact results."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+
+    say("scales off alignment", lens, dim)
+    rng = np.random.default_rng(dim)
+    table, pages = make_table(rng, lens, 32)
+    shape = (pages, 2, 32)
+    code = torch.from_numpy(2.0 ** rng.integers(-2, 3, (*shape, dim))).float().cuda()
+    k, v = torch.zeros_like(code).to(torch.float8_e4m3fn), code.to(torch.float8_e4m3fn)
+    vs = torch.from_numpy(2.0 ** rng.integers(-2, 3, shape)).float().cuda()
+    q = torch.from_numpy(rng.standard_normal((len(lens), 6, dim)).astype(np.float32)).cuda()
+    table_gpu, lens_gpu = torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+
+    def moved(t):
+        buf = torch.empty(t.numel() + 1, device="cuda")
+        buf[1:] = t.flatten()
+        return buf[1:].view(t.shape)
+
+    near, off = (sdq.KVCache(k, v, a, b) for a, b in ((vs, vs), (moved(vs), moved(vs))))
+    assert near.v_scale.data_ptr() % 16 == 0 and off.v_scale.data_ptr() % 16 == 4
+    want, got = (sdq.attn_decode(q, c, table_gpu, lens_gpu, max_len=max(lens)) for c in (near, off))
+    assert torch.equal(got, want)
+    page, at = table[0][np.arange(lens[0]) // 32], np.arange(lens[0]) % 32
+    mean = (code * vs[..., None]).double()[page, :, at].mean(0)
+    assert torch.all((got[0].double().view(2, 3, dim) - mean[:, None]).abs() <= 4 * U * mean[:, None])
