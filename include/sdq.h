@@ -96,7 +96,8 @@ enum {
 enum { SDQ_ORDER_LARGE = 0, SDQ_ORDER_SMALL = 1 };
 /* Inlier scale format (sdq_config.sfmt_i). */
 enum { SDQ_SCALE_DEFAULT = 0, SDQ_SCALE_E4M3 = 1, SDQ_SCALE_UE6M2 = 2 };
-enum { SDQ_DTYPE_F32 = 0, SDQ_DTYPE_BF16 = 1, SDQ_DTYPE_E4M3 = 2 /* caches only */ };
+enum { SDQ_DTYPE_F32 = 0, SDQ_DTYPE_BF16 = 1, SDQ_DTYPE_E4M3 = 2 /* caches, and codes of activations */,
+       SDQ_DTYPE_INT8 = 3 /* codes of activations only */ };
 /* sdq_gemm_ex / sdq_gemm_ws kernel choice. */
 enum { SDQ_PATH_AUTO = 0, SDQ_PATH_DECODE = 1, SDQ_PATH_MFMA = 2, SDQ_PATH_DENSE = 3, SDQ_PATH_SPLITK = 4 };
 
@@ -610,6 +611,106 @@ typedef struct {
 sdq_status sdq_cache_evict_workspace_size(const sdq_kv_cache* cache, int64_t B, int64_t max_len,
                                           int64_t budget, size_t* bytes);
 sdq_status sdq_cache_evict(const sdq_kv_cache* cache, const sdq_evict_args* args, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Between a block's products: sdq_block_norm adds a block's output to the
+ * residual stream and norms the stream for the next projections, sdq_glu_act is
+ * the activation between the projections of a feed-forward block, and
+ * sdq_gemm_int8 the product of a layer that is kept dense.  The first two write
+ * activations, or the 8-bit codes and scales that a product reads.
+ *
+ * out_dtype SDQ_DTYPE_F32 or SDQ_DTYPE_BF16: activations (bf16 to nearest even).
+ * SDQ_DTYPE_INT8 or SDQ_DTYPE_E4M3: one code per element and one fp32 scale per
+ * row, s = amax / qmax and code = v * ((1 / amax) * qmax) to the nearest even
+ * (qmax 127 or 448): the Xq and s_a of the INT and MX families, int8 also those of
+ * sdq_gemm_int8.  They are sdq_quantize_act's of the same fp32 row but for
+ *   - the factor, which there is the quotient qmax / amax: it is one rounding
+ *     apart at most, and a few codes in ten million go to the other neighbour;
+ *   - a row whose factor would pass fp32's range: the codes are those of the row
+ *     times 2^60;
+ *   - a row that holds an infinity or a NaN: its scale is not finite, its codes
+ *     are zero.
+ *
+ * Rows are 16-byte aligned: pointers, and strides times the element size, are
+ * multiples of 16 bytes; strides are in elements.  out is contiguous.  Outputs
+ * overlap no input but where it is said.  M = 0 is a no-op; M below 2^22.
+ * Deterministic.
+ * ------------------------------------------------------------------------ */
+
+/* The norms around a block, and the stream between them:
+ *   u  = y, or norm(y; post_weight, post_bias, post_eps)
+ *   r' = residual + (u * gate) * scale
+ *   n  = norm(r'; weight, bias, eps)
+ *   norm(v; w, b, eps) = d * (1 / sqrt(mean(d^2) + eps)) * w + b,
+ *                        d = v (layer = 0) or v - mean(v) (layer = 1)
+ *   residual  device, M rows of K elements, F32 or BF16
+ *   y         device, the block's output, M rows of K elements, F32 or BF16; or
+ *             NULL: n is the norm of residual (gate, post_weight and residual_out
+ *             NULL)
+ *   gate      device, F32 or BF16, or NULL.  gate_per_row = 0: rows of K elements,
+ *             gate_stride apart (0: one row for all tokens); 1: one element per
+ *             token, gate_stride apart, of any alignment
+ *   weight, bias, post_weight, post_bias  device, fp32 [K].  weight NULL: no n, out
+ *             NULL; post_weight NULL: y is not normed.  The biases are for layer =
+ *             1, or NULL.
+ *   residual_out  device, r' in residual's type, to nearest even; may be residual
+ *             itself, with its stride.  n is that of r' before this rounding.
+ *   out, scales   device, [M][K] codes or activations of n; fp32 [M], with codes
+ * Means, mean squares and the reciprocal root are fp64 (the root is rounded to
+ * fp32), every other step one fp32 operation in the order written.  K is a
+ * multiple of 8, up to 2^22. */
+typedef struct {
+  const void *residual, *y, *gate;
+  const float *weight, *bias, *post_weight, *post_bias;
+  void *residual_out, *out;
+  float* scales;
+  int64_t M, K, residual_stride, y_stride, gate_stride, residual_out_stride;
+  double eps, post_eps;
+  int32_t residual_dtype, y_dtype, gate_dtype, out_dtype, gate_per_row, layer;
+  float scale;
+} sdq_norm_args;
+sdq_status sdq_block_norm(const sdq_norm_args* args, void* stream);
+
+/* The activation of a feed-forward block: h = act(g) * u (gated) or act(g).
+ *   x       device, M rows, F32 or BF16: F elements g, then with gated = 1 F
+ *           elements u (the output of a stacked gate/up projection)
+ *   act     SDQ_ACT_SILU: g / (1 + exp(-g)); SDQ_ACT_GELU: the tanh form,
+ *           g / (1 + exp(-2 sqrt(2/pi) (g + 0.044715 g^3))); SDQ_ACT_RELU
+ *   out, scales  device, [M][F] codes or activations; fp32 [M], with codes
+ * h is evaluated in fp64 and rounded to fp32 once.  An infinity or a NaN in x
+ * reaches its element as an infinity, a NaN or, where g is -inf, a zero.  F is a
+ * multiple of 8, up to 2^22; M * F up to 2^34. */
+enum { SDQ_ACT_SILU = 0, SDQ_ACT_GELU = 1, SDQ_ACT_RELU = 2 };
+typedef struct {
+  const void* x;
+  void* out;
+  float* scales;
+  int64_t M, F, x_stride;
+  int32_t x_dtype, out_dtype, act, gated;
+} sdq_glu_args;
+sdq_status sdq_glu_act(const sdq_glu_args* args, void* stream);
+
+/* The dense product of int8 codes:
+ *   Y[m,n] = sum_k xq[m,k] wq[n,k] * s_x[m] * s_w[n] + bias[n]
+ *   xq    device, M rows of K codes; s_x: fp32 [M] (sdq_quantize_act with int8
+ *         activations, sdq_block_norm or sdq_glu_act write both)
+ *   wq    device, N rows of K codes; s_w: fp32 [N].  sdq_quantize_act of the
+ *         weights' rows gives both, once: no further layout.
+ *   bias  device, fp32 [N], or NULL
+ *   y     device, M rows of N elements, y_stride apart, F32 or BF16 (nearest even),
+ *         aligned to its element
+ * The sum is exact in int32; it is rounded to fp32 and multiplied by s_x, then by
+ * s_w, then the bias is added, each an fp32 operation.  K is a multiple of 16
+ * below 2^17, N up to 2^21, M up to 2^24, M * N up to 2^34; x_stride and w_stride
+ * are multiples of 16 up to 2^22, y_stride up to 2^21. */
+typedef struct {
+  const void *xq, *wq;
+  const float *s_x, *s_w, *bias;
+  void* y;
+  int64_t M, N, K, x_stride, w_stride, y_stride;
+  int32_t y_dtype;
+} sdq_int8_args;
+sdq_status sdq_gemm_int8(const sdq_int8_args* args, void* stream);
 
 #ifdef __cplusplus
 }

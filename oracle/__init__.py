@@ -16,9 +16,11 @@ Quantization for LLM Inference"):
 * ``accounting`` the analytic throughput and bits-per-weight counts of
                  Sections 3.1-3.3 and 5.1;
 * ``decode``     the operators on the key-value cache (head norms, rotation and
-                 append, attention of one token, eviction) in fp64.
+                 append, attention of one token, eviction) in fp64;
+* ``block``      the operators between a block's products (norms and stream, the
+                 activation, the dense int8 product) in fp64 and step by step.
 
 It shares no code with the HIP path.  It is pinned by ``tests/test_oracle_*``
 against closed forms, format definitions, brute force and invariants.
 """
-from . import accounting, decode, formats, sdq  # noqa: F401
+from . import accounting, block, decode, formats, sdq  # noqa: F401

@@ -569,5 +569,9 @@ def gemm_path(cfg: Config, M: int, N: int, K: int, workspace: bool = False) -> i
 from .kv import (KVCache, attn_decode, attn_decode_workspace_size, cache_evict, cache_evict_workspace_size,  # noqa: E402
                  qkv_append)
 
+# The operators between a block's products, and the dense int8 product.
+from .block import block_norm, gemm_int8, glu_act  # noqa: E402
+
+__all__ += ["block_norm", "glu_act", "gemm_int8"]
 __all__ += ["KVCache", "qkv_append", "attn_decode", "attn_decode_workspace_size", "cache_evict",
             "cache_evict_workspace_size"]

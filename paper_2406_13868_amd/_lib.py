@@ -20,7 +20,8 @@ METRIC_MAGNITUDE, METRIC_PRODUCT = 0, 1
 DECOMP = {"same": 0, "magnitude": 1, "product": 2, "error": 3, "output_error": 4}
 ORDER = {"large": 0, "small": 1}
 SCALE = {"": 0, "e4m3": 1, "ue6m2": 2}
-DTYPE_F32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_E4M3, DTYPE_INT8 = 0, 1, 2, 3
+ACT = {"silu": 0, "gelu": 1, "relu": 2}
 PATH_AUTO, PATH_DECODE, PATH_MFMA, PATH_DENSE, PATH_SPLITK = 0, 1, 2, 3, 4
 
 # Every exported symbol, as declared in include/sdq.h.
@@ -32,6 +33,7 @@ EXPORTS = (
     "sdq_unpack_weights", "sdq_gemm_unpacked", "sdq_linear_ws",
     "sdq_qkv_append", "sdq_attn_decode_workspace_size", "sdq_attn_decode",
     "sdq_cache_evict_workspace_size", "sdq_cache_evict",
+    "sdq_block_norm", "sdq_glu_act", "sdq_gemm_int8",
 )
 STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
@@ -69,6 +71,24 @@ class sdq_attn_args(C.Structure):
 class sdq_evict_args(C.Structure):
     _fields_ = [(n, _PTR) for n in ("page_table", "seq_lens", "lens_out", "position_out", "weight_out", "workspace")] + [
         ("ws_bytes", C.c_size_t)] + [(n, _I64) for n in ("B", "table_stride", "max_pages", "max_len", "budget", "recent")]
+
+
+class sdq_norm_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("residual", "y", "gate", "weight", "bias", "post_weight", "post_bias", "residual_out", "out",
+                                    "scales")] + [
+        (n, _I64) for n in ("M", "K", "residual_stride", "y_stride", "gate_stride", "residual_out_stride")] + [
+        ("eps", C.c_double), ("post_eps", C.c_double)] + [
+        (n, _I32) for n in ("residual_dtype", "y_dtype", "gate_dtype", "out_dtype", "gate_per_row", "layer")] + [("scale", C.c_float)]
+
+
+class sdq_glu_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("x", "out", "scales")] + [(n, _I64) for n in ("M", "F", "x_stride")] + [
+        (n, _I32) for n in ("x_dtype", "out_dtype", "act", "gated")]
+
+
+class sdq_int8_args(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("xq", "wq", "s_x", "s_w", "bias", "y")] + [
+        (n, _I64) for n in ("M", "N", "K", "x_stride", "w_stride", "y_stride")] + [("y_dtype", _I32)]
 
 
 class SDQError(RuntimeError):
@@ -153,6 +173,9 @@ def lib() -> C.CDLL:
             "sdq_attn_decode": (C.c_int, [vp, vp, vp]),
             "sdq_cache_evict_workspace_size": (C.c_int, [vp, i64, i64, i64, P(C.c_size_t)]),
             "sdq_cache_evict": (C.c_int, [vp, vp, vp]),
+            "sdq_block_norm": (C.c_int, [vp, vp]),
+            "sdq_glu_act": (C.c_int, [vp, vp]),
+            "sdq_gemm_int8": (C.c_int, [vp, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -43,6 +43,10 @@ SOURCES = [
     "kv_append.hip",
     "attn_decode.hip",
     "cache_evict.hip",
+    "abi_block.hip",
+    "block_norm.hip",
+    "glu_act.hip",
+    "gemm_int8.hip",
 ]
 
 COMMON = [

@@ -1,0 +1,255 @@
+// The norms around a block's products, with the residual stream between them:
+//
+//   u = y, or norm(y; post_weight, post_bias)
+//   r' = r + (u * gate) * scale                    (written in r's type)
+//   n = norm(r'; weight, bias)                     (of r' before that rounding)
+//   norm(v) = d * (1 / sqrt(mean d^2 + eps)) * w + b,  d = v (rms) or v - mean v (layer)
+//
+// n leaves as activations or as 8-bit codes with a scale per row (row_ops.h).
+// Sums over a row and the reciprocal root are in fp64, everything else is one
+// fp32 operation after the other: what the order of a sum could change is lost in
+// the rounding of the root, so that the codes of a row are the same however many
+// threads share it.  (Their cost hides behind the loads.)
+//
+// A row is held in registers by a wave or a workgroup, in pieces of eight
+// elements, and read and written once.  Rows of more than kMostHeld elements are
+// read again for each sum instead.
+#include <hip/hip_runtime.h>
+
+#include "row_ops.h"
+
+#pragma clang fp contract(off)
+
+namespace sdq {
+namespace {
+
+constexpr uint32_t kMostHeld = 32768;
+
+// What a row needs of the arguments, its pointers' types decided at run time:
+// the branches are uniform.
+struct Row {
+  const NormArgs& a;
+  int64_t m;
+  float gate_of_row;
+  __device__ __forceinline__ Row(const NormArgs& args, int64_t row) : a(args), m(row), gate_of_row(1.f) {
+    if (a.gate && !a.gate_cols)
+      gate_of_row = a.gate_type == kF32 ? static_cast<const float*>(a.gate)[m * a.gate_stride]
+                                        : __uint_as_float(uint32_t(static_cast<const uint16_t*>(a.gate)[m * a.gate_stride]) << 16);
+  }
+  // r += (u * gate) * scale for the eight elements from k
+  __device__ __forceinline__ void join(int64_t k, const float (&u)[8], float (&r)[8]) const {
+    float g[8];
+    if (a.gate && a.gate_cols) {
+      load8(a.gate_type, a.gate, m * a.gate_stride + k, g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = gate_of_row;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = u[i] * g[i];
+      r[i] = r[i] + t * a.scale;
+    }
+  }
+};
+
+// v = d * rstd * w + b for the eight elements from k, d = v - mean
+__device__ __forceinline__ void apply(float (&v)[8], double mean, float rstd, const float* w, const float* b, int64_t k) {
+  float g[8];
+  load8<true>(w, k, g);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float d = float(double(v[i]) - mean);
+    v[i] = d * rstd * g[i];
+  }
+  if (b) {
+    load8<true>(b, k, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] + g[i];
+  }
+}
+
+__device__ __forceinline__ float root(double sum, uint32_t K, double eps) { return float(1.0 / sqrt(sum / double(K) + eps)); }
+
+template <int NT, int CH>
+struct Held {
+  float v[CH][8];
+};
+
+// Mean (layer only) and reciprocal root of a held row.
+template <int NT, int CH>
+__device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint32_t P, const NormArgs& a, double eps, double* red,
+                                      double& mean, float& rstd) {
+  mean = 0.0;
+  if (a.layer) {
+    double s = 0.0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += double(v[c][i]);  // 0 past the row
+    mean = row_sum<NT>(s, red) / double(a.K);
+  }
+  double s = 0.0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double d = double(v[c][i]) - mean;
+        s = __builtin_fma(d, d, s);
+      }
+  rstd = root(row_sum<NT>(s, red + NT / 64), a.K, eps);
+}
+
+template <bool XF32, int NT, int CH>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArgs a) {
+  __shared__ double red[4 * (NT / 64)];
+  __shared__ uint32_t top[NT / 64];
+  const uint32_t t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, P = a.K / 8;
+  const int64_t m = NT == 64 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
+  if (m >= a.M) return;  // whole waves, and none that others wait for
+  const Row row(a, m);
+  float r[CH][8] = {};
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P) load8<XF32>(a.residual, m * a.residual_stride + (t + c * NT) * 8, r[c]);
+  if (a.y_type != kNone) {
+    float u[CH][8] = {};
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (t + c * NT < P) load8(a.y_type, a.y, m * a.y_stride + (t + c * NT) * 8, u[c]);
+    if (a.post_weight) {
+      double mean;
+      float rstd;
+      stats<NT, CH>(u, t, P, a, a.post_eps, red, mean, rstd);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (t + c * NT < P) apply(u[c], mean, rstd, a.post_weight, a.post_bias, (t + c * NT) * 8);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (t + c * NT < P) {
+        row.join((t + c * NT) * 8, u[c], r[c]);
+        store8(XF32, a.residual_out, m * a.residual_out_stride + (t + c * NT) * 8, r[c]);
+      }
+  }
+  if (!a.weight) return;
+  double mean;
+  float rstd;
+  stats<NT, CH>(r, t, P, a, a.eps, red + 2 * (NT / 64), mean, rstd);
+  uint32_t most = 0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P) {
+      apply(r[c], mean, rstd, a.weight, a.bias, (t + c * NT) * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, abs_bits(r[c][i]));
+    }
+  const int64_t to = m * a.K;
+  if (a.out_type == kF32 || a.out_type == kBF16) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (t + c * NT < P) store8(a.out_type == kF32, a.out, to + (t + c * NT) * 8, r[c]);
+    return;
+  }
+  const bool e4m3 = a.out_type == kE4M3;
+  const RowCode code(row_umax<NT>(most, top), e4m3);
+  if (t == 0) a.scales[m] = code.s;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P)
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + to + (t + c * NT) * 8) = codes8(r[c], code, e4m3);
+}
+
+// Rows of any width: each sum reads the row again.  The stream is written in the
+// last pass, which reads an element before it writes it, so it may be in place.
+__global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
+  constexpr int NT = 1024;
+  __shared__ double red[4][NT / 64];
+  __shared__ uint32_t top[NT / 64];
+  const int64_t m = blockIdx.x, K = a.K;
+  const Row row(a, m);
+  double post_mean = 0.0, mean = 0.0;
+  float post_rstd = 1.f, rstd = 1.f;
+  auto block_out = [&](int64_t k, float (&u)[8]) { load8(a.y_type, a.y, m * a.y_stride + k, u); };
+  auto stream = [&](int64_t k, float (&r)[8]) {
+    load8(a.x_type, a.residual, m * a.residual_stride + k, r);
+    if (a.y_type == kNone) return;
+    float u[8];
+    block_out(k, u);
+    if (a.post_weight) apply(u, post_mean, post_rstd, a.post_weight, a.post_bias, k);
+    row.join(k, u, r);
+  };
+  auto sums = [&](auto&& values, double eps, double* red0, double* red1, double& mu, float& root_of) {
+    if (a.layer) {
+      double s = 0.0;
+      for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
+        float v[8];
+        values(k, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += double(v[i]);
+      }
+      mu = row_sum<NT>(s, red0) / double(a.K);
+    }
+    double s = 0.0;
+    for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
+      float v[8];
+      values(k, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double d = double(v[i]) - mu;
+        s = __builtin_fma(d, d, s);
+      }
+    }
+    root_of = root(row_sum<NT>(s, red1), a.K, eps);
+  };
+  if (a.y_type != kNone && a.post_weight) sums(block_out, a.post_eps, red[0], red[1], post_mean, post_rstd);
+  const bool coded = a.weight && (a.out_type == kInt8 || a.out_type == kE4M3), e4m3 = a.out_type == kE4M3;
+  uint32_t most = 0;
+  if (a.weight) {
+    sums(stream, a.eps, red[2], red[3], mean, rstd);
+    if (coded)
+      for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
+        float v[8];
+        stream(k, v);
+        apply(v, mean, rstd, a.weight, a.bias, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(v[i]));
+      }
+  }
+  const RowCode code(coded ? row_umax<NT>(most, top) : 0u, e4m3);
+  if (coded && threadIdx.x == 0) a.scales[m] = code.s;
+  for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
+    float v[8];
+    stream(k, v);
+    if (a.y_type != kNone) store8(a.x_type == kF32, a.residual_out, m * a.residual_out_stride + k, v);
+    if (!a.weight) continue;
+    apply(v, mean, rstd, a.weight, a.bias, k);
+    if (coded) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + m * K + k) = codes8(v, code, e4m3);
+    else store8(a.out_type == kF32, a.out, m * K + k, v);
+  }
+}
+
+template <int NT, int CH>
+void launch(const NormArgs& a, hipStream_t st) {
+  const dim3 grid(NT == 64 ? (a.M + 3) / 4 : a.M), block(NT == 64 ? 256 : NT);
+  if (a.x_type == kF32) hipLaunchKernelGGL((block_norm_kernel<true, NT, CH>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((block_norm_kernel<false, NT, CH>), grid, block, 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(const NormArgs& a, hipStream_t st) {
+  const uint32_t P = a.K / 8;
+  if (P <= 64) launch<64, 1>(a, st);
+  else if (P <= 128) launch<64, 2>(a, st);
+  else if (P <= 256) launch<256, 1>(a, st);
+  else if (P <= 512) launch<256, 2>(a, st);
+  else if (P <= 1024) launch<1024, 1>(a, st);
+  else if (P <= 2048) launch<1024, 2>(a, st);
+  else if (a.K <= kMostHeld) launch<1024, 4>(a, st);
+  else hipLaunchKernelGGL(block_norm_wide, dim3(a.M), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace sdq

@@ -1,0 +1,174 @@
+// The activation between the projections of a feed-forward block:
+//
+//   h = act(g) * u (gated: x's rows are g, then u)  or  act(g)
+//   silu: g / (1 + exp(-g));  relu: max(g, 0)
+//   gelu: g / (1 + exp(-2 sqrt(2 / pi) (g + 0.044715 g^3))), the tanh form
+//
+// h leaves as activations or as 8-bit codes with a scale per row (row_ops.h).  It
+// is evaluated in fp64 and rounded to fp32 once: two evaluations of exp that
+// differ in an fp32's last bit would give other codes now and then.
+#include <hip/hip_runtime.h>
+
+#include "row_ops.h"
+#include "sdq.h"
+
+#pragma clang fp contract(off)
+
+namespace sdq {
+namespace {
+
+constexpr uint32_t kMostHeld = 32768;
+
+// exp(t) within 1e-14 of itself for |t| <= 700: t = n ln 2 + r with |r| <= ln 2 / 2,
+// exp(r) by its series up to r^11 / 11! (the next term is 6e-15), times 2^n.
+__device__ __forceinline__ double exp64(double t) {
+  const double n = __builtin_rint(t * 1.4426950408889634);
+  double r = __builtin_fma(n, -0.6931471805599453, t);
+  r = __builtin_fma(n, -2.3190468138462996e-17, r);  // ln 2 less its fp64
+  double p = 1.0 / 39916800;
+  p = __builtin_fma(p, r, 1.0 / 3628800);
+  p = __builtin_fma(p, r, 1.0 / 362880);
+  p = __builtin_fma(p, r, 1.0 / 40320);
+  p = __builtin_fma(p, r, 1.0 / 5040);
+  p = __builtin_fma(p, r, 1.0 / 720);
+  p = __builtin_fma(p, r, 1.0 / 120);
+  p = __builtin_fma(p, r, 1.0 / 24);
+  p = __builtin_fma(p, r, 1.0 / 6);
+  p = __builtin_fma(p, r, 0.5);
+  p = __builtin_fma(p, r, 1.0);
+  p = __builtin_fma(p, r, 1.0);
+  return __builtin_ldexp(p, int(n));
+}
+
+// g / (1 + exp(t)).  t is held to where exp is finite: at the upper end the
+// quotient is below fp32's least number, at the lower it is g.
+__device__ __forceinline__ double gate64(double g, double t) {
+  t = fmin(fmax(t, -700.0), 700.0);
+  const double q = 1.0 + exp64(t);
+  double x = __builtin_amdgcn_rcp(q);
+  x = __builtin_fma(x, __builtin_fma(-q, x, 1.0), x);  // Newton's steps for 1 / q
+  x = __builtin_fma(x, __builtin_fma(-q, x, 1.0), x);
+  return g * x;
+}
+
+template <int ACT>
+__device__ __forceinline__ double act64(double g) {
+  if constexpr (ACT == SDQ_ACT_SILU) return gate64(g, -g);
+  if constexpr (ACT == SDQ_ACT_GELU) return gate64(g, -1.5957691216057308 * (g + 0.044715 * (g * g * g)));
+  return g > 0.0 || g != g ? g : 0.0;
+}
+
+// h of the eight elements from k of a row
+template <int ACT, bool XF32, bool GATED>
+__device__ __forceinline__ void values(const GluArgs& a, int64_t row, int64_t k, float (&h)[8]) {
+  float g[8], u[8];
+  load8<XF32>(a.x, row + k, g);
+  if constexpr (GATED) load8<XF32>(a.x, row + a.F + k, u);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    double v = act64<ACT>(double(g[i]));
+    if constexpr (GATED) v = v * double(u[i]);
+    h[i] = float(v);
+  }
+}
+
+template <int ACT, bool XF32, bool GATED, int NT, int CH>
+__global__ __launch_bounds__(NT) void glu_code_kernel(GluArgs a) {
+  __shared__ uint32_t top[NT / 64];
+  const uint32_t t = threadIdx.x, P = a.F / 8;
+  const int64_t m = blockIdx.x, from = m * a.x_stride;
+  const bool e4m3 = a.out_type == kE4M3;
+  float h[CH][8] = {};
+  uint32_t most = 0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P) {
+      values<ACT, XF32, GATED>(a, from, (t + c * NT) * 8, h[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, abs_bits(h[c][i]));
+    }
+  const RowCode code(row_umax<NT>(most, top), e4m3);
+  if (t == 0) a.scales[m] = code.s;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (t + c * NT < P)
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + m * a.F + (t + c * NT) * 8) = codes8(h[c], code, e4m3);
+}
+
+// Rows of any width: the activation is evaluated for the maximum and again for
+// the codes.
+template <int ACT, bool XF32, bool GATED>
+__global__ __launch_bounds__(1024) void glu_code_wide(GluArgs a) {
+  constexpr int NT = 1024;
+  __shared__ uint32_t top[NT / 64];
+  const int64_t m = blockIdx.x, from = m * a.x_stride;
+  const bool e4m3 = a.out_type == kE4M3;
+  uint32_t most = 0;
+  for (int64_t k = threadIdx.x * 8; k < a.F; k += NT * 8) {
+    float h[8];
+    values<ACT, XF32, GATED>(a, from, k, h);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, abs_bits(h[i]));
+  }
+  const RowCode code(row_umax<NT>(most, top), e4m3);
+  if (threadIdx.x == 0) a.scales[m] = code.s;
+  for (int64_t k = threadIdx.x * 8; k < a.F; k += NT * 8) {
+    float h[8];
+    values<ACT, XF32, GATED>(a, from, k, h);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + m * a.F + k) = codes8(h, code, e4m3);
+  }
+}
+
+// Activations: no row has to wait for its maximum, so a thread takes the piece
+// that its index names.
+template <int ACT, bool XF32, bool GATED>
+__global__ __launch_bounds__(256) void glu_act_kernel(GluArgs a) {
+  const uint32_t P = a.F / 8;
+  const uint64_t at = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t m = uint32_t(at / P), p = uint32_t(at - uint64_t(m) * P);
+  if (m >= a.M) return;
+  float h[8];
+  values<ACT, XF32, GATED>(a, int64_t(m) * a.x_stride, int64_t(p) * 8, h);
+  store8(a.out_type == kF32, a.out, int64_t(m) * a.F + int64_t(p) * 8, h);
+}
+
+template <int ACT, bool XF32, bool GATED>
+void launch(const GluArgs& a, hipStream_t st) {
+  const uint32_t P = a.F / 8;
+  if (a.out_type == kF32 || a.out_type == kBF16) {
+    const uint64_t pieces = uint64_t(a.M) * P;
+    hipLaunchKernelGGL((glu_act_kernel<ACT, XF32, GATED>), dim3(uint32_t((pieces + 255) / 256)), dim3(256), 0, st, a);
+  } else if (P <= 256) {
+    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 256, 1>), dim3(a.M), dim3(256), 0, st, a);
+  } else if (P <= 512) {
+    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 256, 2>), dim3(a.M), dim3(256), 0, st, a);
+  } else if (P <= 1024) {
+    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 1>), dim3(a.M), dim3(1024), 0, st, a);
+  } else if (P <= 2048) {
+    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 2>), dim3(a.M), dim3(1024), 0, st, a);
+  } else if (a.F <= kMostHeld) {
+    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 4>), dim3(a.M), dim3(1024), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((glu_code_wide<ACT, XF32, GATED>), dim3(a.M), dim3(1024), 0, st, a);
+  }
+}
+
+template <int ACT>
+void launch_act(const GluArgs& a, hipStream_t st) {
+  const bool f32 = a.x_type == kF32;
+  if (f32 && a.gated) launch<ACT, true, true>(a, st);
+  else if (f32) launch<ACT, true, false>(a, st);
+  else if (a.gated) launch<ACT, false, true>(a, st);
+  else launch<ACT, false, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_glu_act(const GluArgs& a, hipStream_t st) {
+  if (a.act == SDQ_ACT_SILU) launch_act<SDQ_ACT_SILU>(a, st);
+  else if (a.act == SDQ_ACT_GELU) launch_act<SDQ_ACT_GELU>(a, st);
+  else launch_act<SDQ_ACT_RELU>(a, st);
+  return hipGetLastError();
+}
+
+}  // namespace sdq

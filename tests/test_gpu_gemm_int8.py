@@ -1,0 +1,144 @@
+"""GPU: the dense int8 product against exact integer sums."""
+import numpy as np
+import pytest
+
+from block_util import equal, rounded
+from gpu_util import say, torch_cuda
+from oracle import block as O
+
+pytestmark = pytest.mark.gpu
+
+
+def make(torch, seed, M, N, K, x_gap=0, w_gap=0, least=-127, bias=True):
+    """Codes with other codes between the rows, scales and a bias, on the GPU and the host."""
+    rng = np.random.default_rng(seed)
+    x, w = rng.integers(least, 128, (M, K + x_gap)).astype(np.int8), rng.integers(least, 128, (N, K + w_gap)).astype(np.int8)
+    sx, sw, b = (rng.uniform(0.5, 2, n).astype(np.float32) / 100 for n in (M, N, N))
+    b = b * 1000 if bias else None
+    g = [torch.from_numpy(t).cuda() for t in (x, sx, w, sw)]
+    return (g[0][:, :K], g[1], g[2][:, :K], g[3]), None if b is None else torch.from_numpy(b).cuda(), (x[:, :K], sx, w[:, :K], sw), b
+
+
+def steps(host, b):
+    """fp32(sum) * s_x * s_w + bias, an fp32 operation each: the result's every bit."""
+    _, total = O.product64(*host)
+    y = total.astype(np.float32) * host[1][:, None] * host[3]
+    return y if b is None else y + b
+
+
+def check(torch, sdq, seed, M, N, K, dtype=None, **kw):
+    say(M, N, K, dtype, kw)
+    args, bias, host, b = make(torch, seed, M, N, K, **kw)
+    y = sdq.gemm_int8(*args, bias=bias, out_dtype=dtype)
+    want = steps(host, b)
+    assert y.shape == (M, N) and equal(y.float().cpu().numpy(), rounded(torch, want, y.dtype)), (M, N, K)
+    y64, _ = O.product64(*host, b)
+    size = np.abs(y64 - (0 if b is None else b)) * 3 + np.abs(y64)  # the sum's rounding and two products', and the bias's
+    assert (np.abs(want - y64) <= 1.01 * O.U * size).all()
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 7, 8, 9, 15, 16, 17, 31, 32, 33, 48, 63, 64, 65, 96, 127, 128, 129, 191, 256, 257, 300])
+def test_every_number_of_tokens(M):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    check(torch, sdq, M, M, 200, 400)
+    check(torch, sdq, M, M, 77, 1104, torch.bfloat16, x_gap=16, w_gap=32)
+
+
+@pytest.mark.parametrize("K", [16, 32, 48, 64, 112, 128, 144, 240, 256, 272, 368, 512, 528, 1008, 1024, 1040, 2032, 2048, 2064, 4080, 4096, 4112, 8208])
+def test_every_kind_of_depth(K):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    for M, N in ((1, 33), (3, 64), (9, 130), (40, 65), (140, 257)):
+        check(torch, sdq, K, M, N, K, [torch.bfloat16, torch.float32][K // 16 % 2], bias=M % 2 == 0)
+
+
+@pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 1000, 1023])
+def test_every_number_of_outputs(N):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    for M in (1, 6, 20, 70, 260):
+        check(torch, sdq, N, M, N, 272, [torch.bfloat16, torch.float32][M % 2])
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (4, 4096, 4096), (16, 4096, 4096), (64, 4096, 4096), (200, 4096, 4096), (517, 5003, 1104),
+                                   (1024, 2048, 4096), (2100, 1300, 272)])
+def test_sizes_that_fill_the_gpu(M, N, K):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    check(torch, sdq, 11, M, N, K, torch.bfloat16)
+
+
+@pytest.mark.parametrize("M", [1, 8, 24, 130])
+def test_the_largest_sums_are_exact(M):
+    """All codes -128 over the longest K: 2^14 times it, just below 2^31; and sums past 2^24, which fp32 rounds."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    K = (1 << 17) - 16
+    say(M, K)
+    for a, b in ((-128, -128), (-128, 127), (127, 127)):
+        x = torch.full((M, K), a, dtype=torch.int8, device="cuda")
+        w = torch.full((35, K), b, dtype=torch.int8, device="cuda")
+        x[:, 5] += 1 if a < 0 else -1
+        y = sdq.gemm_int8(x, torch.ones(M, device="cuda"), w, torch.ones(35, device="cuda"))
+        total = K * a * b + (b if a < 0 else -b)
+        assert (y.cpu().numpy() == np.float32(total)).all() and abs(total) < 2 ** 31
+
+
+def test_strided_outputs_and_what_lies_beside_them():
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    for M, N in ((1, 37), (5, 64), (30, 100), (150, 300)):
+        for dt in (torch.float32, torch.bfloat16):
+            say(M, N, dt)
+            args, bias, host, b = make(torch, M, M, N, 160)
+            big = torch.full((M + 2, N + 11), 7.0, dtype=dt, device="cuda")
+            y = sdq.gemm_int8(*args, bias=bias, out=big[:M, 3:3 + N])
+            assert y.data_ptr() == big[:, 3:].data_ptr()
+            assert equal(y.float().cpu().numpy(), rounded(torch, steps(host, b), dt))
+            big[:M, 3:3 + N] = 7
+            assert (big == 7).all()
+
+
+def test_codes_of_the_other_operators_and_the_scales_of_bad_rows():
+    """uint8 codes as quantize_act writes them; a scale that is not finite reaches its row's outputs."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    cfg = sdq.Config.int_family()
+    X, W = torch.randn((9, 96), device="cuda"), torch.randn((50, 96), device="cuda")
+    xq, sx = sdq.quantize_act(X, cfg)
+    wq, sw = sdq.quantize_act(W, cfg)
+    y = sdq.gemm_int8(xq, sx, wq, sw)
+    host = [t.cpu().numpy() for t in (xq.view(torch.int8), sx, wq.view(torch.int8), sw)]
+    assert equal(y.cpu().numpy(), steps(host, None))
+    for M in (3, 40, 200):
+        sx = torch.ones(M, device="cuda")
+        sx[1] = float("nan")
+        x = torch.zeros((M, 96), dtype=torch.uint8, device="cuda")
+        y = sdq.gemm_int8(x, sx, wq, sw)
+        assert y[1].isnan().all() and (y[[0] + list(range(2, M))] == 0).all()
+
+
+def test_calls_without_rows_and_calls_that_are_refused():
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    x, w = torch.zeros((3, 64), dtype=torch.int8, device="cuda"), torch.zeros((5, 64), dtype=torch.int8, device="cuda")
+    s3, s5 = torch.ones(3, device="cuda"), torch.ones(5, device="cuda")
+    assert sdq.gemm_int8(x[:0], s3[:0], w, s5).shape == (0, 5)
+
+    def refused(match, *a, **kw):
+        with pytest.raises((ValueError, sdq.SDQError), match=match):
+            sdq.gemm_int8(*a, **kw)
+
+    refused("int8 codes", x.float(), s3, w, s5)
+    refused("int8 codes", x, s3, w.short(), s5)
+    refused("wq must be", x, s3, w[:, :48], s5)
+    refused("s_x must be", x, s5, w, s5)
+    refused("s_w must be", x, s3, w, s3)
+    refused("bias must be", x, s3, w, s5, bias=s3)
+    refused("bias must be", x, s3, w, s5, bias=s5.double())
+    refused("out must be", x, s3, w, s5, out=torch.zeros((3, 4), device="cuda"))
+    refused("float32 or bfloat16", x, s3, w, s5, out_dtype=torch.float16)
+    refused("SHAPE", x[:, :40], s3, w[:, :40], s5)
+    refused("SHAPE", x[:, 1:49], s3, w[:, :48], s5)
+    refused("contiguous", x.t().contiguous().t(), s3, w, s5)
