@@ -5,6 +5,9 @@
 // not depend on how K is divided.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cstdint>
+
 #include "block.h"
 #include "kernels.h"
 #include "tile_out.h"
@@ -19,30 +22,61 @@ typedef int i16v __attribute__((ext_vector_type(16)));
 
 constexpr int kChunk = 128;  // bytes of K per row and stage: whole cache lines
 
-// 16 bytes per lane to shared memory, lane i's at `to` + 16 i.
+// Weights that are read once pass the caches by.
+constexpr int kStream = 2;
+
+// 16 bytes per lane to shared memory, lane i's at `to` + 16 i.  In assembly, and
+// awaited by the kernels themselves: a read of shared memory waits for every request
+// that the compiler knows of and cannot tell from it, and it loses count where a loop
+// closes (256 x 4096 x 4096: 13.0 us that way, 10.5 this).  The instruction returns
+// nothing to registers; nothing else here uses m0.
+template <int HINT = 0>
 __device__ __forceinline__ void request_1k(__amdgpu_buffer_rsrc_t from, uint8_t* to, uint32_t at, uint32_t base) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, at, base, 0, 0);
+  const uint32_t where = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)to));
+  if constexpr (HINT == kStream)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen nt lds" ::"v"(at), "s"(from), "s"(where), "s"(base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen lds" ::"v"(at), "s"(from), "s"(where), "s"(base) : "memory");
 }
 
-// A workgroup owns BM tokens x BN outputs, each wave WM x WN of them in tiles of
-// 32 x 32.  Chunks of 128 bytes of K go to shared memory directly, the next one
-// while this one is used; each stage is an array of its own, so that the compiler
-// can tell a read of one from the requests into the other.  Rows past the end are
-// the last row again (their results are not stored), and the pieces of 16 past the
-// end of K are the last piece again, with zeros in their place on the tokens' side.
+// s_waitcnt's operand: at most n vector memory operations on their way, and no
+// operation on shared memory.
+constexpr int wait_vm(int n) { return (n & 15) | (n >> 4) << 14 | 0x0070; }
+
+// An offset outside every buffer here: such a load reads nothing.
+constexpr uint32_t kNowhere = 0x80000000u;
+
+// What no kernel writes while this one runs, for scalar loads.
+__device__ __forceinline__ const __attribute__((address_space(4))) float* constant(const float* p) {
+  return (const __attribute__((address_space(4))) float*)(p);
+}
+
+// All waves' operations on shared memory are done; requests from memory go on.
+__device__ __forceinline__ void barrier_lds() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---- tiles -----------------------------------------------------------------
+// BM tokens from m0 x BN outputs from n0 by a workgroup, each wave WM x WN of them in
+// tiles of 32 x 32.  Chunks of 128 bytes of K go to shared memory directly, up to
+// STAGES - 1 of them while one is used.  Rows past the end are the last row again
+// (their results are not stored), and the pieces of 16 past the end of K are the last
+// piece again, with zeros in their place on the tokens' side.
 //
 // In a stage, row r's piece p (16 bytes) lies at r * 128 + 16 * (p ^ (r / 2 & 7)):
 // the 16 lanes that read a piece of 16 rows together touch every bank once.
-template <int BM, int BN, int WM, int WN, bool YB>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int8Args a, int m_blocks) {
+template <int BM, int BN, int STAGES>
+constexpr int kTileBytes = STAGES * (BM + BN) * kChunk;
+template <int BM, int BN, int WM, int WN, int STAGES, bool YB>
+__device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, uint8_t* mem) {
   constexpr int kWaves = (BM / WM) * (BN / WN), MS = WM / 32, NS = WN / 32;
   constexpr int kA = BM / 8 / kWaves, kB = BN / 8 / kWaves;  // requests per wave and stage
-  __shared__ __align__(1024) uint8_t s0[(BM + BN) * kChunk], s1[(BM + BN) * kChunk];
+  constexpr int kStage = (BM + BN) * kChunk;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, h = lane >> 5;
-  int group, mblock;
-  square_work(blockIdx.x, gridDim.x / m_blocks, m_blocks, group, mblock);
-  const int m0 = mblock * BM, n0 = group * BN;
   const int rows = min(a.M - m0, BM), outs = min(a.N - n0, BN);
   const int chunks = (a.K + kChunk - 1) / kChunk, last = chunks - 1;
   const int left = a.K - last * kChunk;  // bytes of the last chunk
@@ -56,17 +90,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int
     const int j = i < kA ? i : i - kA, r = (j * kWaves + wave) * 8 + (lane >> 3);
     at[i] = (i < kA ? uint32_t(min(r, rows - 1)) * uint32_t(a.x_stride) : uint32_t(min(r, outs - 1)) * uint32_t(a.w_stride)) + piece(j);
   }
+  // no branch around the requests: as many are on their way at every wait
   const auto request = [&](int c, uint8_t* s) {
-    if (c > last) return;
 #pragma unroll
     for (int i = 0; i < kA + kB; ++i) {
       const int j = i < kA ? i : i - kA;
-      uint32_t v = at[i];
-      if (c == last) {
-        const int p = piece(j);
-        v += min(p, left - 16) - p;
-      }
-      request_1k(i < kA ? xr : wr, s + (i < kA ? 0 : BM * kChunk) + (j * kWaves + wave) * 1024, v, uint32_t(c) * kChunk);
+      const uint32_t v = c > last ? kNowhere : at[i] + (c == last ? min(piece(j), left - 16) - piece(j) : 0);
+      request_1k(i < kA ? xr : wr, s + (i < kA ? 0 : BM * kChunk) + (j * kWaves + wave) * 1024, v, uint32_t(min(c, last)) * kChunk);
     }
   };
 
@@ -82,33 +112,59 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int
 #pragma unroll
   for (int s = 0; s < 4; ++s) from[s] = col * kChunk + (((2 * s + h) ^ (col >> 1 & 7)) << 4);
 
-  const auto step = [&](int c, const uint8_t* s, uint8_t* next) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's requests of chunk c
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();  // every wave's; and the other stage has been read
-    asm volatile("" ::: "memory");
-    request(c + 1, next);
+  struct Step { i4 a[MS], b[NS]; };
+  Step f[2];
+  const auto read = [&](const uint8_t* s, int t, Step& to) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      i4 A[MS], B[NS];
+    for (int j = 0; j < NS; ++j) to.b[j] = *reinterpret_cast<const i4*>(s + (BM + wn + j * 32) * kChunk + from[t]);
 #pragma unroll
-      for (int i = 0; i < MS; ++i) {
-        A[i] = *reinterpret_cast<const i4*>(s + (wm + i * 32) * kChunk + from[t]);
-        if (c == last && (2 * t + h) * 16 >= left) A[i] = i4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int j = 0; j < NS; ++j) B[j] = *reinterpret_cast<const i4*>(s + (BM + wn + j * 32) * kChunk + from[t]);
-#pragma unroll
-      for (int i = 0; i < MS; ++i)
-#pragma unroll
-        for (int j = 0; j < NS; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(A[i], B[j], acc[i][j], 0, 0, 0);
-    }
+    for (int i = 0; i < MS; ++i) to.a[i] = *reinterpret_cast<const i4*>(s + (wm + i * 32) * kChunk + from[t]);
   };
-  request(0, s0);
-  for (int c = 0; c < chunks; c += 2) {
-    step(c, s0, s1);
-    if (c + 1 < chunks) step(c + 1, s1, s0);
+  const auto multiply = [&](const Step& x) {
+#pragma unroll
+    for (int i = 0; i < MS; ++i)
+#pragma unroll
+      for (int j = 0; j < NS; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.a[i], x.b[j], acc[i][j], 0, 0, 0);
+  };
+  // Chunk c, requested into s, has arrived there for every wave; and every wave has
+  // read what it reads of the chunk before.
+  const auto arrive = [&](int c, uint8_t* s) {
+    __builtin_amdgcn_s_waitcnt(wait_vm((STAGES - 2) * (kA + kB)));  // the chunks behind it may be on their way
+    if (c == last && left < kChunk) {
+#pragma unroll
+      for (int i = 0; i < kA; ++i)
+        if (piece(i) >= left) *reinterpret_cast<i4*>(s + (i * kWaves + wave) * 1024 + lane * 16) = i4{0, 0, 0, 0};
+    }
+    barrier_lds();
+  };
+  // Each step's operands are read while the step before is multiplied, and the next
+  // chunk is awaited before the last step, so that a chunk begins on operands in
+  // registers.
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) request(i, mem + i * kStage);
+  arrive(0, mem);
+  request(STAGES - 1, mem + (STAGES - 1) * kStage);
+  read(mem, 0, f[0]);
+  for (int c = 0;;) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) {  // the stage's place is a constant of the reads
+      uint8_t *const s = mem + i * kStage, *const next = mem + (i + 1) % STAGES * kStage;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (t == 3) {
+          arrive(c + 1, next);
+          request(c + STAGES, s);
+        }
+        read(t < 3 ? s : next, (t + 1) & 3, f[(t + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f[t & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (++c == chunks) goto multiplied;
+    }
   }
+multiplied:
+  __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no request into shared memory outlives the workgroup
 
   const RowScales<MS> rs = load_row_scales<MS>(a.s_x, a.M, m0 + wm, h);
   const uint32_t es = YB ? 2 : 4;
@@ -134,17 +190,243 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int
   }
 }
 
-template <int BM, int BN, int WM, int WN>
-hipError_t tile(const Int8Args& a, hipStream_t st) {
-  const int mb = (a.M + BM - 1) / BM, nb = (a.N + BN - 1) / BN;
-  const dim3 grid(unsigned(mb) * unsigned(nb)), block((BM / WM) * (BN / WN) * 64);
-  if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, true>), grid, block, 0, st, a, mb);
-  else hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, false>), grid, block, 0, st, a, mb);
+template <int BM, int BN, int WM, int WN, int STAGES, bool YB>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int8Args a, int m_blocks) {
+  __shared__ __align__(1024) uint8_t mem[kTileBytes<BM, BN, STAGES>];
+  int group, mblock;
+  square_work(blockIdx.x, gridDim.x / m_blocks, m_blocks, group, mblock);
+  tile_product<BM, BN, WM, WN, STAGES, YB>(a, mblock * BM, group * BN, mem);
+}
+
+// ---- few tokens ------------------------------------------------------------
+// Up to 64 tokens, whose time is that of the weights' bytes.  A workgroup takes one
+// tile of 16 outputs and all tokens after the other; its waves take a tile's
+// 128-byte units of K in turn, and their sums meet in shared memory.  A wave waits
+// for the others at the end of a tile only, with the next tile's units on their way.
+//
+// Whole pieces of rows are requested, into registers, DEPTH units ahead: there is
+// more room than in shared memory, and loads return in order, so that tokens, which
+// the L2 holds, would wait for weights requested before them.  From there they pass
+// through shared memory of the wave's own into the operands' order.  (Requested in
+// that order, lanes that follow each other take four rows, which costs the address
+// units three times as much: 2.9 TB/s with 16 tokens, 1.4 with 64.)
+//
+// 16x16x64: A = 16 rows of W, B = 16 tokens, 16 bytes of K a lane (lane l: row or
+// token l & 15, bytes 16 (l >> 4)); the sums leave a lane four outputs of a token.
+// XG: groups of 8 tokens.
+template <int XG, int NT, int WAVES, bool YB>
+__global__ __launch_bounds__(WAVES * 64) void gemm_int8_few(Int8Args a) {
+  constexpr int MT = (XG + 1) / 2, NR = NT * 16, kRows = NR + MT * 16;  // rows of a unit in shared memory, weights first
+  constexpr int kUnit = (2 * NT + XG) * 1024;  // what a unit requests: the half of a tile of 16 tokens that is not there stays what it was
+  constexpr int kRing = WAVES * kUnit + (kRows * kChunk - kUnit);
+  __shared__ __align__(1024) uint8_t ring[3 * kRing];
+  __shared__ int sums[MT * NT * 4 * 64];  // of all waves: whole numbers, whose order does not matter
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g = lane >> 4;
+  const int units = (a.K + kChunk - 1) / kChunk, left = a.K - (units - 1) * kChunk;
+  const int tiles = (a.N + NR - 1) / NR;
+  // this wave's units of a tile: one at least, which past the end of K counts for nothing
+  const int per = max((units - wave + WAVES - 1) / WAVES, 1);
+  const int mine = per * ((tiles - int(blockIdx.x) + int(gridDim.x) - 1) / int(gridDim.x));
+
+  // Row r's piece p (16 bytes) lies at r * 128 + 16 * (p ^ (r / 2 & 7)); the lanes
+  // write their pieces side by side, so they load them in that order.
+  const auto piece = [&](int r) { return ((lane & 7) ^ (r >> 1 & 7)) * 16; };
+  // the pieces past the end of K are the last piece again
+  const auto inside = [&](int unit, uint32_t at, int r) { return unit < units - 1 ? at : at + min(piece(r), left - 16) - piece(r); };
+
+  // the next unit to request, and the lane's place in its tile's rows
+  int next_tile = blockIdx.x, next_unit = wave, next_count = 0;
+  __amdgpu_buffer_rsrc_t wr;
+  uint32_t w_at[2 * NT], x_at[XG];
+  const auto w_rows = [&] {
+    // rows past the end are the last one again; their results are not stored
+    const int outs = min(a.N - next_tile * NR, NR);
+    wr = buffer_rsrc(a.w + next_tile * NR * a.w_stride, uint32_t((outs - 1) * a.w_stride + a.K));
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) w_at[i] = uint32_t(min(i * 8 + (lane >> 3), outs - 1)) * uint32_t(a.w_stride) + piece(i * 8 + (lane >> 3));
+  };
+  const __amdgpu_buffer_rsrc_t xr = buffer_rsrc(a.x, uint32_t((a.M - 1) * a.x_stride + a.K));
+#pragma unroll
+  for (int i = 0; i < XG; ++i) x_at[i] = uint32_t(min(i * 8 + (lane >> 3), a.M - 1)) * uint32_t(a.x_stride) + piece(i * 8 + (lane >> 3));
+  // Requests have no branch around them, so that as many are on their way at every
+  // wait; those past the last unit lie outside the buffer and read nothing.
+  const auto request = [&](int j, uint8_t* to) {
+    const int unit = min(next_unit, units - 1);
+    const uint32_t base = uint32_t(unit) * kChunk;
+    to += wave * kUnit;
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i)
+      request_1k<kStream>(wr, to + i * 1024, j < mine ? inside(unit, w_at[i], i * 8 + (lane >> 3)) : kNowhere, base);
+#pragma unroll
+    for (int i = 0; i < XG; ++i)
+      request_1k(xr, to + (2 * NT + i) * 1024, j < mine ? inside(unit, x_at[i], i * 8 + (lane >> 3)) : kNowhere, base);
+    next_unit += WAVES;
+    if (++next_count == per) {
+      next_count = 0;
+      next_unit = wave;
+      if (j + 1 < mine) {
+        next_tile += gridDim.x;
+        w_rows();
+      }
+    }
+  };
+
+  i4 acc[MT * NT];
+#pragma unroll
+  for (int t = 0; t < MT * NT; ++t) acc[t] = i4{0, 0, 0, 0};
+  uint32_t from[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) from[s] = i16 * kChunk + (((4 * s + g) ^ (i16 >> 1 & 7)) << 4);
+
+  // the sums of the waves, by the first MT of them: a tile of 16 tokens each
+  int tile = blockIdx.x, unit = wave, count = 0;
+  constexpr int kSums = (MT * NT + WAVES - 1) / WAVES;
+  float sx[kSums];
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) {
+    const int m = (wave + i * WAVES) / NT * 16 + i16;
+    sx[i] = m < a.M ? a.s_x[m] : 0.f;
+  }
+  // The four values of the lane's outputs, by scalar loads: a vector load would
+  // wait for the requests before it.
+  const auto of_lane = [&](const float* p, int nt, float (&v)[4]) {
+    const __attribute__((address_space(4))) float* q = constant(p);
+    float all[16];
+    const int first = tile * NR + nt * 16;
+    if (first + 16 <= a.N) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) all[i] = q[first + i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) all[i] = q[min(first + i, a.N - 1)];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = g < 2 ? (g == 0 ? all[e] : all[4 + e]) : (g == 2 ? all[8 + e] : all[12 + e]);
+  };
+  const auto finish = [&] {
+#pragma unroll
+    for (int t = 0; t < MT * NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __hip_atomic_fetch_add(&sums[(t * 4 + e) * 64 + lane], acc[t][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        acc[t][e] = 0;
+      }
+    barrier_lds();
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) {
+      const int p = wave + i * WAVES, nt = p % NT, m = p / NT * 16 + i16;
+      if (p >= MT * NT) break;
+      int s[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] = sums[(p * 4 + e) * 64 + lane];
+        sums[(p * 4 + e) * 64 + lane] = 0;
+      }
+      const int n = tile * NR + nt * 16 + 4 * g;
+      float sw[4], bias[4] = {};
+      of_lane(a.s_w, nt, sw);
+      if (a.bias) of_lane(a.bias, nt, bias);
+      if (m < a.M) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < a.N) {
+            float y = float(s[e]) * sx[i] * sw[e];
+            if (a.bias) y += bias[e];
+            store_y(a.y, YB, m * a.y_stride + n + e, y);
+          }
+      }
+    }
+    barrier_lds();
+    tile += gridDim.x;
+    unit = wave;
+    count = 0;
+  };
+
+  for (int i = threadIdx.x; i < MT * NT * 4 * 64; i += WAVES * 64) sums[i] = 0;
+  barrier_lds();
+  w_rows();
+  request(0, ring);
+  request(1, ring + kRing);
+  uint8_t *now = ring, *free = ring + 2 * kRing;  // unit j, and where unit j - 1 was
+  for (int j = 0; j < mine; ++j) {
+    __builtin_amdgcn_s_waitcnt(wait_vm(2 * NT + XG));  // unit j + 1 may be on its way
+    __builtin_amdgcn_sched_barrier(0);
+    request(j + 2, free);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint8_t* mem = now + wave * kUnit;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      i4 b[NT], v[MT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        b[t] = *reinterpret_cast<const i4*>(mem + t * 16 * kChunk + from[s]);
+        if (unit >= units - 1 && (unit >= units || s * 64 + g * 16 >= left)) b[t] = i4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) v[t] = *reinterpret_cast<const i4*>(mem + (NT + t) * 16 * kChunk + from[s]);
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int r = 0; r < NT; ++r) acc[t * NT + r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[r], v[t], acc[t * NT + r], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    free = now;
+    now = now + kRing < ring + 3 * kRing ? now + kRing : ring;
+    unit += WAVES;
+    if (++count == per) finish();
+  }
+  __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no request into shared memory outlives the workgroup
+}
+
+template <int XG, int NT, int WAVES>
+hipError_t few(const Int8Args& a, int groups, hipStream_t st) {
+  const dim3 grid(unsigned(std::min((a.N + 16 * NT - 1) / (16 * NT), groups))), block(WAVES * 64);
+  if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_few<XG, NT, WAVES, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((gemm_int8_few<XG, NT, WAVES, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
+template <int BM, int BN, int WM, int WN, int STAGES>
+hipError_t tile(const Int8Args& a, hipStream_t st) {
+  const int mb = (a.M + BM - 1) / BM, nb = (a.N + BN - 1) / BN;
+  const dim3 grid(unsigned(mb) * unsigned(nb)), block((BM / WM) * (BN / WN) * 64);
+  if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, STAGES, true>), grid, block, 0, st, a, mb);
+  else hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, STAGES, false>), grid, block, 0, st, a, mb);
+  return hipGetLastError();
+}
+
+// Time of a form of tiles, in microseconds: in every round of 256 compute units, or
+// twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2 for its
+// beginning and end.  Fitted to products of 128 to 4096 tokens by 4096 outputs, K =
+// 4096.
+struct Form {
+  int bm, bn;
+  float one, two;
+  double time(const Int8Args& a) const {
+    const double chunks = (a.K + kChunk - 1) / kChunk;
+    const int64_t tiles = int64_t((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn), round = two > 0 ? 512 : 256;
+    const double whole = chunks * (two > 0 ? two : one) + 2, part = chunks * one + 2;
+    const int64_t rest = tiles % round;
+    return double(tiles / round) * whole + (rest == 0 ? 0 : rest <= 256 ? part : whole);
+  }
+};
+
 }  // namespace
 
-hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) { return tile<128, 128, 64, 64>(a, st); }
+hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
+  if (a.M <= 8) return few<1, 1, 8>(a, 512, st);
+  if (a.M <= 16) return a.N < 16384 ? few<2, 1, 8>(a, 256, st) : few<2, 2, 4>(a, 512, st);
+  if (a.M <= 32 && a.N <= 8192) return few<4, 1, 8>(a, 256, st);
+  const double t[5] = {Form{64, 64, .22f, .41f}.time(a), Form{64, 128, .37f, .69f}.time(a), Form{128, 128, .60f, 0.f}.time(a),
+                       Form{128, 128, .80f, 1.1f}.time(a), Form{256, 256, 1.85f, 0.f}.time(a)};
+  switch (std::min_element(t, t + 5) - t) {
+    case 0: return tile<64, 64, 32, 32, 4>(a, st);
+    case 1: return tile<64, 128, 32, 32, 3>(a, st);
+    case 2: return tile<128, 128, 64, 32, 4>(a, st);
+    case 3: return tile<128, 128, 64, 64, 2>(a, st);
+    default: return tile<256, 256, 128, 64, 2>(a, st);
+  }
+}
 
 }  // namespace sdq
