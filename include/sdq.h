@@ -699,6 +699,10 @@ sdq_status sdq_glu_act(const sdq_glu_args* args, void* stream);
  *   bias  device, fp32 [N], or NULL
  *   y     device, M rows of N elements, y_stride apart, F32 or BF16 (nearest even),
  *         aligned to its element
+ *   workspace device, 16-byte aligned, at least sdq_gemm_int8_workspace_size bytes
+ *         (0 for many shapes), or NULL: where the outputs alone do not fill the GPU,
+ *         K is divided over more workgroups with it, whose sums a second kernel
+ *         adds.  The result is the same bit for bit.  Scratch, as in sdq_gemm_ws.
  * The sum is exact in int32; it is rounded to fp32 and multiplied by s_x, then by
  * s_w, then the bias is added, each an fp32 operation.  K is a multiple of 16
  * below 2^17, N up to 2^21, M up to 2^24, M * N up to 2^34; x_stride and w_stride
@@ -706,10 +710,12 @@ sdq_status sdq_glu_act(const sdq_glu_args* args, void* stream);
 typedef struct {
   const void *xq, *wq;
   const float *s_x, *s_w, *bias;
-  void* y;
+  void *y, *workspace;
+  size_t ws_bytes;
   int64_t M, N, K, x_stride, w_stride, y_stride;
   int32_t y_dtype;
 } sdq_int8_args;
+sdq_status sdq_gemm_int8_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes);
 sdq_status sdq_gemm_int8(const sdq_int8_args* args, void* stream);
 
 #ifdef __cplusplus

@@ -570,8 +570,8 @@ from .kv import (KVCache, attn_decode, attn_decode_workspace_size, cache_evict, 
                  qkv_append)
 
 # The operators between a block's products, and the dense int8 product.
-from .block import block_norm, gemm_int8, glu_act  # noqa: E402
+from .block import block_norm, gemm_int8, gemm_int8_workspace_size, glu_act  # noqa: E402
 
-__all__ += ["block_norm", "glu_act", "gemm_int8"]
+__all__ += ["block_norm", "glu_act", "gemm_int8", "gemm_int8_workspace_size"]
 __all__ += ["KVCache", "qkv_append", "attn_decode", "attn_decode_workspace_size", "cache_evict",
             "cache_evict_workspace_size"]

@@ -33,7 +33,7 @@ EXPORTS = (
     "sdq_unpack_weights", "sdq_gemm_unpacked", "sdq_linear_ws",
     "sdq_qkv_append", "sdq_attn_decode_workspace_size", "sdq_attn_decode",
     "sdq_cache_evict_workspace_size", "sdq_cache_evict",
-    "sdq_block_norm", "sdq_glu_act", "sdq_gemm_int8",
+    "sdq_block_norm", "sdq_glu_act", "sdq_gemm_int8_workspace_size", "sdq_gemm_int8",
 )
 STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
@@ -87,7 +87,7 @@ class sdq_glu_args(C.Structure):
 
 
 class sdq_int8_args(C.Structure):
-    _fields_ = [(n, _PTR) for n in ("xq", "wq", "s_x", "s_w", "bias", "y")] + [
+    _fields_ = [(n, _PTR) for n in ("xq", "wq", "s_x", "s_w", "bias", "y", "workspace")] + [("ws_bytes", C.c_size_t)] + [
         (n, _I64) for n in ("M", "N", "K", "x_stride", "w_stride", "y_stride")] + [("y_dtype", _I32)]
 
 
@@ -175,6 +175,7 @@ def lib() -> C.CDLL:
             "sdq_cache_evict": (C.c_int, [vp, vp, vp]),
             "sdq_block_norm": (C.c_int, [vp, vp]),
             "sdq_glu_act": (C.c_int, [vp, vp]),
+            "sdq_gemm_int8_workspace_size": (C.c_int, [i64, i64, i64, P(C.c_size_t)]),
             "sdq_gemm_int8": (C.c_int, [vp, vp]),
         }
         for name, (res, args) in sig.items():

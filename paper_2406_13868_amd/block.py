@@ -9,14 +9,16 @@ is done by the library's kernels.
 """
 from __future__ import annotations
 
+import ctypes as C
+import functools
 import struct
 
-from . import _dev, _empty, _lib, _need, _stream, _torch
+from . import _dev, _empty, _lib, _need, _need_bytes, _stream, _torch, _workspace
 
 # The argument structures as bytes, as in kv.py.
 _NORM = struct.Struct("@10P6q2d6if0q")
 _GLU = struct.Struct("@3P3q4i0q")
-_INT8 = struct.Struct("@6P6qi0q")
+_INT8 = struct.Struct("@7PN6qi0q")
 _CODES = {"int8": _lib.DTYPE_INT8, "e4m3": _lib.DTYPE_E4M3}
 
 
@@ -191,14 +193,23 @@ def glu_act(x, act: str = "silu", gated: bool = True, out_dtype=None, out=None, 
     return out, scales
 
 
-def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, stream=None):
+@functools.lru_cache(maxsize=4096)
+def gemm_int8_workspace_size(M: int, N: int, K: int) -> int:
+    """Device workspace bytes that gemm_int8 takes for these sizes (0: none)."""
+    n = C.c_size_t()
+    _lib.check(_lib.lib().sdq_gemm_int8_workspace_size(M, N, K, C.byref(n)), "sdq_gemm_int8_workspace_size")
+    return n.value
+
+
+def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
     """The dense product of int8 codes, Y = s_x * (xq @ wq^T) * s_w + bias: returns Y [M, N].
 
     xq [M, K] and wq [N, K] are codes as int8, or as the uint8 that quantize_act,
     block_norm and glu_act write (rows may be strided); s_x fp32 [M], s_w fp32 [N],
     bias fp32 [N].  The codes and scales of a weight are quantize_act(W, cfg) with
     int8 activations, once.  out: [M, N], fp32 or bf16, rows may be strided; or
-    out_dtype (default fp32)."""
+    out_dtype (default fp32).  workspace: a uint8 tensor of gemm_int8_workspace_size
+    bytes, or a fresh one is made where that is not 0."""
     torch = _torch()
     x_ld, x_at = _rows(xq, "xq")
     M, K = xq.shape
@@ -215,7 +226,15 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, stream=None
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise ValueError(f"out must be {out_dtype}")
     y_ld, y_at = _rows(out, "out", M, N, index)
+    need = gemm_int8_workspace_size(M, N, K)
+    ws = ws_bytes = 0
+    if need:
+        if workspace is None:
+            workspace = _workspace(need, xq.device, stream)
+        elif _need_bytes(workspace, need, "workspace").get_device() != index:
+            raise ValueError(f"workspace is on another device: {workspace.device}")
+        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
     _run("sdq_gemm_int8", M, _INT8.pack(
-        x_at, w_at, _vec(s_x, M, "s_x", index), _vec(s_w, N, "s_w", index), _vec(bias, N, "bias", index), y_at, M, N, K, x_ld, w_ld,
+        x_at, w_at, _vec(s_x, M, "s_x", index), _vec(s_w, N, "s_w", index), _vec(bias, N, "bias", index), y_at, ws, ws_bytes, M, N, K, x_ld, w_ld,
         y_ld, _type(out, "out")), index, stream)
     return out

@@ -120,21 +120,34 @@ extern "C" sdq_status sdq_glu_act(const sdq_glu_args* t, void* stream) {
   return launch_glu_act(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SDQ_OK : SDQ_ERR_HIP;
 }
 
+namespace {
+// The bounds keep int32 sums exact and every offset within a tile below 2^32.
+bool int8_fits(int64_t M, int64_t N, int64_t K) {
+  return M >= 0 && M <= (int64_t(1) << 24) && N >= 1 && N <= (int64_t(1) << 21) && K >= 16 && K % 16 == 0 && K < (int64_t(1) << 17) &&
+         M <= (int64_t(1) << 34) / N;
+}
+}  // namespace
+
+extern "C" sdq_status sdq_gemm_int8_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes) {
+  if (!bytes) return SDQ_ERR_NULL;
+  if (!int8_fits(M, N, K)) return SDQ_ERR_SHAPE;
+  *bytes = M ? gemm_int8_workspace_bytes(M, N, K) : 0;
+  return SDQ_OK;
+}
+
 extern "C" sdq_status sdq_gemm_int8(const sdq_int8_args* t, void* stream) {
   if (!t) return SDQ_ERR_NULL;
   if (!activations(t->y_dtype)) return SDQ_ERR_CONFIG;
   const int64_t M = t->M, N = t->N, K = t->K;
-  // the bounds keep int32 sums exact and every offset within a tile below 2^32
-  if (M < 0 || M > (int64_t(1) << 24) || N < 1 || N > (int64_t(1) << 21) || K < 16 || K % 16 || K >= (int64_t(1) << 17) ||
-      M > (int64_t(1) << 34) / N)
-    return SDQ_ERR_SHAPE;
+  if (!int8_fits(M, N, K)) return SDQ_ERR_SHAPE;
   if (M == 0) return SDQ_OK;
   if (!t->xq || !t->wq || !t->s_x || !t->s_w || !t->y) return SDQ_ERR_NULL;
   const int64_t lim = int64_t(1) << 22;
   if (!rows_fit(t->xq, SDQ_DTYPE_INT8, t->x_stride, K) || !rows_fit(t->wq, SDQ_DTYPE_INT8, t->w_stride, K) || t->x_stride > lim ||
       t->w_stride > lim || t->y_stride < N || t->y_stride > (int64_t(1) << 21) ||
-      reinterpret_cast<uintptr_t>(t->y) % size_t(bytes_of(t->y_dtype)))
+      reinterpret_cast<uintptr_t>(t->y) % size_t(bytes_of(t->y_dtype)) || !aligned16(t->workspace))
     return SDQ_ERR_SHAPE;
+  if (t->workspace && t->ws_bytes < gemm_int8_workspace_bytes(M, N, K)) return SDQ_ERR_BUFFER_TOO_SMALL;
   Int8Args a;
   a.x = static_cast<const int8_t*>(t->xq);
   a.w = static_cast<const int8_t*>(t->wq);
@@ -149,6 +162,7 @@ extern "C" sdq_status sdq_gemm_int8(const sdq_int8_args* t, void* stream) {
   a.N = int32_t(N);
   a.K = int32_t(K);
   a.y_bf16 = t->y_dtype == SDQ_DTYPE_BF16;
+  a.ws = t->workspace;
   drop_pending_error();
   return launch_gemm_int8(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SDQ_OK : SDQ_ERR_HIP;
 }

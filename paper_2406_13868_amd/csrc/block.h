@@ -43,7 +43,9 @@ struct Int8Args {
   int64_t x_stride, w_stride, y_stride;  // elements
   int32_t M, N, K;
   bool y_bf16;
+  void* ws;  // gemm_int8_workspace_bytes bytes, or NULL: K is not divided
 };
+size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st);
 
 }  // namespace sdq

@@ -59,6 +59,8 @@ __device__ __forceinline__ void barrier_lds() {
   asm volatile("" ::: "memory");
 }
 
+constexpr int kSums = 4;  // beside kF32 and kBF16: int32 sums, not scaled yet
+
 // ---- tiles -----------------------------------------------------------------
 // BM tokens from m0 x BN outputs from n0 by a workgroup, each wave WM x WN of them in
 // tiles of 32 x 32.  Chunks of 128 bytes of K go to shared memory directly, up to
@@ -70,7 +72,7 @@ __device__ __forceinline__ void barrier_lds() {
 // the 16 lanes that read a piece of 16 rows together touch every bank once.
 template <int BM, int BN, int STAGES>
 constexpr int kTileBytes = STAGES * (BM + BN) * kChunk;
-template <int BM, int BN, int WM, int WN, int STAGES, bool YB>
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
 __device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, uint8_t* mem) {
   constexpr int kWaves = (BM / WM) * (BN / WN), MS = WM / 32, NS = WN / 32;
   constexpr int kA = BM / 8 / kWaves, kB = BN / 8 / kWaves;  // requests per wave and stage
@@ -166,36 +168,76 @@ __device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, 
 multiplied:
   __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no request into shared memory outlives the workgroup
 
-  const RowScales<MS> rs = load_row_scales<MS>(a.s_x, a.M, m0 + wm, h);
-  const uint32_t es = YB ? 2 : 4;
+  const uint32_t es = OUT == kBF16 ? 2 : 4;
   const int have = min(a.M - m0 - wm, WM);
   if (have <= 0) return;
   const __amdgpu_buffer_rsrc_t yr =
       buffer_rsrc(static_cast<uint8_t*>(a.y) + ((m0 + wm) * a.y_stride) * es, uint32_t((have - 1) * a.y_stride + a.N) * es);
+  RowScales<MS> rs;
+  if constexpr (OUT != kSums) rs = load_row_scales<MS>(a.s_x, a.M, m0 + wm, h);
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     const int n = n0 + wn + j * 32 + col;
     if (n >= a.N) continue;
-    const float sw = a.s_w[n], b = a.bias ? a.bias[n] : 0.f;
+    float sw = 0.f, b = 0.f;
+    if constexpr (OUT != kSums) {
+      sw = a.s_w[n];
+      if (a.bias) b = a.bias[n];
+    }
 #pragma unroll
     for (int i = 0; i < MS; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float v = float(acc[i][j][e]) * rs.v[i][e] * sw;
-        if (a.bias) v += b;
         const uint32_t idx = uint32_t(i * 32 + tile_row(e, h)) * uint32_t(a.y_stride) + uint32_t(n);
-        if constexpr (YB) __builtin_amdgcn_raw_buffer_store_b16(bf16_bits(v), yr, idx * 2u, 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), yr, idx * 4u, 0, 0);
+        if constexpr (OUT == kSums) {
+          __builtin_amdgcn_raw_buffer_store_b32(uint32_t(acc[i][j][e]), yr, idx * 4u, 0, 0);
+        } else {
+          float v = float(acc[i][j][e]) * rs.v[i][e] * sw;
+          if (a.bias) v += b;
+          if constexpr (OUT == kBF16) __builtin_amdgcn_raw_buffer_store_b16(bf16_bits(v), yr, idx * 2u, 0, 0);
+          else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), yr, idx * 4u, 0, 0);
+        }
       }
   }
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool YB>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int8Args a, int m_blocks) {
+// part: chunks of K that a workgroup multiplies.  With OUT = kSums the sums of part p
+// go to a.y, an int32 [parts][M][N].
+template <int BM, int BN, int WM, int WN, int STAGES, int OUT>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void gemm_int8_tile(Int8Args a, int m_blocks, int groups, int part) {
   __shared__ __align__(1024) uint8_t mem[kTileBytes<BM, BN, STAGES>];
-  int group, mblock;
-  square_work(blockIdx.x, gridDim.x / m_blocks, m_blocks, group, mblock);
-  tile_product<BM, BN, WM, WN, STAGES, YB>(a, mblock * BM, group * BN, mem);
+  int group, mblock, b = blockIdx.x;
+  if constexpr (OUT == kSums) {
+    const int p = b / (m_blocks * groups);
+    b -= p * (m_blocks * groups);
+    a.x += int64_t(p) * part * kChunk;
+    a.w += int64_t(p) * part * kChunk;
+    a.y = static_cast<int32_t*>(a.y) + int64_t(p) * a.M * a.N;
+    a.K = min(a.K - p * part * kChunk, part * kChunk);
+  }
+  square_work(b, groups, m_blocks, group, mblock);
+  tile_product<BM, BN, WM, WN, STAGES, OUT>(a, mblock * BM, group * BN, mem);
+}
+
+// The sums of the parts, scaled: V neighbouring outputs a thread.
+template <int V, bool YB>
+__global__ __launch_bounds__(256) void gemm_int8_join(Int8Args a, const int32_t* sums, int parts) {
+  const uint32_t per = uint32_t(a.N) / V;
+  const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t m = uint32_t(i / per), n = uint32_t(i - uint64_t(m) * per) * V;
+  if (m >= uint32_t(a.M)) return;
+  typedef int vec __attribute__((ext_vector_type(V)));
+  const int64_t all = int64_t(a.M) * a.N;
+  const int32_t* p = sums + int64_t(m) * a.N + n;
+  vec s = *reinterpret_cast<const vec*>(p);
+  for (int k = 1; k < parts; ++k) s += *reinterpret_cast<const vec*>(p + k * all);
+  const float sx = a.s_x[m];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    float y = float(s[e]) * sx * a.s_w[n + e];
+    if (a.bias) y += a.bias[n + e];
+    store_y(a.y, YB, m * a.y_stride + n + e, y);
+  }
 }
 
 // ---- few tokens ------------------------------------------------------------
@@ -388,45 +430,96 @@ hipError_t few(const Int8Args& a, int groups, hipStream_t st) {
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES>
-hipError_t tile(const Int8Args& a, hipStream_t st) {
+hipError_t tile(const Int8Args& a, int parts, hipStream_t st) {
   const int mb = (a.M + BM - 1) / BM, nb = (a.N + BN - 1) / BN;
-  const dim3 grid(unsigned(mb) * unsigned(nb)), block((BM / WM) * (BN / WN) * 64);
-  if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, STAGES, true>), grid, block, 0, st, a, mb);
-  else hipLaunchKernelGGL((gemm_int8_tile<BM, BN, WM, WN, STAGES, false>), grid, block, 0, st, a, mb);
+  const dim3 block((BM / WM) * (BN / WN) * 64);
+  const auto launch = [&](auto kernel, const Int8Args& args, int k, int part) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(mb) * unsigned(nb) * unsigned(k)), block, 0, st, args, mb, nb, part);
+    return hipGetLastError();
+  };
+  if (parts == 1)
+    return a.y_bf16 ? launch(gemm_int8_tile<BM, BN, WM, WN, STAGES, kBF16>, a, 1, 0) : launch(gemm_int8_tile<BM, BN, WM, WN, STAGES, kF32>, a, 1, 0);
+  Int8Args sums = a;
+  sums.y = a.ws;
+  sums.y_stride = a.N;
+  const int chunks = (a.K + kChunk - 1) / kChunk, part = (chunks + parts - 1) / parts;
+  return launch(gemm_int8_tile<BM, BN, WM, WN, STAGES, kSums>, sums, parts, part);
+}
+
+template <int V>
+hipError_t join(const Int8Args& a, int parts, hipStream_t st) {
+  const dim3 grid(unsigned((int64_t(a.M) * (a.N / V) + 255) / 256)), block(256);
+  const int32_t* sums = static_cast<const int32_t*>(a.ws);
+  if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_join<V, true>), grid, block, 0, st, a, sums, parts);
+  else hipLaunchKernelGGL((gemm_int8_join<V, false>), grid, block, 0, st, a, sums, parts);
   return hipGetLastError();
 }
 
-// Time of a form of tiles, in microseconds: in every round of 256 compute units, or
-// twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2 for its
-// beginning and end.  Fitted to products of 128 to 4096 tokens by 4096 outputs, K =
-// 4096.
-struct Form {
-  int bm, bn;
-  float one, two;
-  double time(const Int8Args& a) const {
-    const double chunks = (a.K + kChunk - 1) / kChunk;
-    const int64_t tiles = int64_t((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn), round = two > 0 ? 512 : 256;
-    const double whole = chunks * (two > 0 ? two : one) + 2, part = chunks * one + 2;
-    const int64_t rest = tiles % round;
-    return double(tiles / round) * whole + (rest == 0 ? 0 : rest <= 256 ? part : whole);
+// The forms of tiles, and their times in microseconds: in every round of 256 compute
+// units, or twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2
+// for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs, K = 4096
+// and, where rows are not whole cache lines and a chunk of each takes two, 4112.
+struct Form { int bm, bn; double one, two, one_odd, two_odd; };
+constexpr Form kForms[] = {{64, 64, .22, .46, .30, .63},
+                           {64, 128, .42, .80, .53, 1.0},
+                           {128, 128, .72, 0, .80, 0},
+                           {128, 128, .87, 1.18, 1.04, 1.46},
+                           {256, 256, 1.85, 0, 2.1, 0}};
+
+struct Choice { int form, parts; };
+
+// K divided over `parts` workgroups costs a second launch and the sums' way through
+// memory: 3 microseconds, and 4 TB/s of them written and read.  (64 x 4096 x 16384:
+// 26.6 us undivided, 17.0 in 4 parts.)
+Choice choose(int64_t M, int64_t N, int64_t K, bool divide) {
+  const int chunks = int((K + kChunk - 1) / kChunk);
+  Choice best{0, 1};
+  double least = 1e30;
+  for (int f = 0; f < int(sizeof(kForms) / sizeof(kForms[0])); ++f) {
+    const Form& m = kForms[f];
+    const int64_t tiles = ((M + m.bm - 1) / m.bm) * ((N + m.bn - 1) / m.bn), round = m.two > 0 ? 512 : 256;
+    const double one = K % kChunk ? m.one_odd : m.one, two = round == 256 ? one : K % kChunk ? m.two_odd : m.two;
+    for (int parts = 1; parts <= (divide && tiles < 512 ? 16 : 1); ++parts) {
+      const int part = (chunks + parts - 1) / parts;
+      if (parts > 1 && (part < 4 || (parts - 1) * part >= chunks || tiles * parts > 2 * round)) continue;
+      const int64_t all = tiles * parts, rest = all % round;
+      const double whole = part * two + 2, some = part * one + 2;
+      double t = double(all / round) * whole + (rest == 0 ? 0 : rest <= 256 ? some : whole);
+      if (parts > 1) t = 1.1 * (t + 3 + double(M) * double(N) * (8 * parts + 4) / 4e6);
+      if (t < least) {
+        least = t;
+        best = {f, parts};
+      }
+    }
   }
-};
+  return best;
+}
+
+bool few_tokens(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 8192); }
 
 }  // namespace
+
+size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  if (few_tokens(M, N)) return 0;
+  const int parts = choose(M, N, K, true).parts;
+  return parts == 1 ? 0 : size_t(M) * size_t(N) * size_t(parts) * 4;
+}
 
 hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
   if (a.M <= 8) return few<1, 1, 8>(a, 512, st);
   if (a.M <= 16) return a.N < 16384 ? few<2, 1, 8>(a, 256, st) : few<2, 2, 4>(a, 512, st);
-  if (a.M <= 32 && a.N <= 8192) return few<4, 1, 8>(a, 256, st);
-  const double t[5] = {Form{64, 64, .22f, .41f}.time(a), Form{64, 128, .37f, .69f}.time(a), Form{128, 128, .60f, 0.f}.time(a),
-                       Form{128, 128, .80f, 1.1f}.time(a), Form{256, 256, 1.85f, 0.f}.time(a)};
-  switch (std::min_element(t, t + 5) - t) {
-    case 0: return tile<64, 64, 32, 32, 4>(a, st);
-    case 1: return tile<64, 128, 32, 32, 3>(a, st);
-    case 2: return tile<128, 128, 64, 32, 4>(a, st);
-    case 3: return tile<128, 128, 64, 64, 2>(a, st);
-    default: return tile<256, 256, 128, 64, 2>(a, st);
+  if (few_tokens(a.M, a.N)) return few<4, 1, 8>(a, 256, st);
+  const Choice c = choose(a.M, a.N, a.K, a.ws != nullptr);
+  hipError_t e;
+  switch (c.form) {
+    case 0: e = tile<64, 64, 32, 32, 4>(a, c.parts, st); break;
+    case 1: e = tile<64, 128, 32, 32, 3>(a, c.parts, st); break;
+    case 2: e = tile<128, 128, 64, 32, 4>(a, c.parts, st); break;
+    case 3: e = tile<128, 128, 64, 64, 2>(a, c.parts, st); break;
+    default: e = tile<256, 256, 128, 64, 2>(a, c.parts, st); break;
   }
+  if (e != hipSuccess || c.parts == 1) return e;
+  return a.N % 4 == 0 ? join<4>(a, c.parts, st) : join<1>(a, c.parts, st);
 }
 
 }  // namespace sdq

@@ -10,7 +10,7 @@ import paper_2406_13868_amd as sdq  # noqa: E402
 from paper_2406_13868_amd import _lib, block  # noqa: E402
 
 P = 1 << 20  # stands for a device pointer in calls that are refused before it is used
-OK, NULL, SHAPE, CONFIG, VALUE = 0, -1, -2, -3, -7
+OK, NULL, SHAPE, CONFIG, SMALL, VALUE = 0, -1, -2, -3, -4, -7
 NAN, INF = float("nan"), float("inf")
 
 
@@ -83,6 +83,20 @@ def test_glu(kw, status):
 ])
 def test_gemm(kw, status):
     assert _gemm(**kw) == status
+
+
+def test_workspaces_of_products():
+    n = C.c_size_t()
+    size = _lib.lib().sdq_gemm_int8_workspace_size
+    assert size(64, 4096, 16384, C.byref(n)) == OK and n.value % (64 * 4096 * 4) == 0 and n.value > 64 * 4096 * 4
+    need = n.value
+    big = dict(M=64, N=4096, K=16384, x_stride=16384, w_stride=16384, y_stride=4096)
+    assert _gemm(workspace=P, ws_bytes=need - 1, **big) == SMALL
+    assert _gemm(workspace=P + 4, ws_bytes=need, **big) == SHAPE
+    assert size(64, 4096, 16384, None) == NULL and size(64, 0, 16, C.byref(n)) == SHAPE and size(64, 5, 24, C.byref(n)) == SHAPE
+    for M in (0, 1, 16, 4096):
+        assert size(M, 4096, 4096, C.byref(n)) == OK and n.value == 0
+    assert sdq.gemm_int8_workspace_size(64, 4096, 16384) == need
 
 
 def _raises(fn, match):

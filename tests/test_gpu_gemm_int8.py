@@ -85,6 +85,39 @@ def test_the_largest_sums_are_exact(M):
         assert (y.cpu().numpy() == np.float32(total)).all() and abs(total) < 2 ** 31
 
 
+DIVIDED = [(64, 4096, 16384), (100, 300, 8208), (40, 37, 13456), (130, 1000, 8192), (33, 4, 4096), (600, 601, 6000)]
+
+
+@pytest.mark.parametrize("M,N,K", DIVIDED)
+def test_products_divided_over_their_depth(M, N, K):
+    """With a workspace, which holds NaN bits before; without one the same bits."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    from paper_2406_13868_amd import _lib, block
+    need = sdq.gemm_int8_workspace_size(M, N, K)
+    parts = need // (4 * M * N)
+    assert parts > 1 and need == 4 * M * N * parts
+    for dt in (torch.float32, torch.bfloat16):
+        say(M, N, K, parts, dt)
+        args, bias, host, b = make(torch, M, M, N, K, x_gap=16 * (N % 2))
+        ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+        big = torch.full((M + 1, N + 5), 7.0, dtype=dt, device="cuda")
+        y = sdq.gemm_int8(*args, bias=bias, out=big[:M, :N], workspace=ws[:need])
+        assert equal(y.float().cpu().numpy(), rounded(torch, steps(host, b), dt))
+        assert (ws[need:] == 0xFF).all() and (big[M:] == 7).all() and (big[:, N:] == 7).all()
+        assert torch.equal(sdq.gemm_int8(*args, bias=bias, out_dtype=dt), y)
+        if not args[0].is_contiguous():
+            continue
+        z = torch.empty((M, N), dtype=dt, device="cuda")
+        call = _lib.sdq_int8_args(xq=args[0].data_ptr(), wq=args[2].data_ptr(), s_x=args[1].data_ptr(), s_w=args[3].data_ptr(),
+                                  bias=bias.data_ptr(), y=z.data_ptr(), M=M, N=N, K=K, x_stride=K, w_stride=K, y_stride=N,
+                                  y_dtype=int(dt is torch.bfloat16))
+        block._run("sdq_gemm_int8", M, bytes(call), 0, None)
+        assert torch.equal(z, y)
+    with pytest.raises(ValueError, match="workspace holds"):
+        sdq.gemm_int8(*args, workspace=ws[: need - 16])
+
+
 def test_strided_outputs_and_what_lies_beside_them():
     torch = torch_cuda()
     import paper_2406_13868_amd as sdq
