@@ -13,62 +13,94 @@ import ctypes as C
 import functools
 import struct
 
-from . import _dev, _empty, _lib, _need, _need_bytes, _stream, _torch, _workspace
+from . import _dev, _empty, _lib, _need, _need_bytes, _torch, _workspace
 
 # The argument structures as bytes, as in kv.py.
 _NORM = struct.Struct("@10P6q2d6if0q")
 _GLU = struct.Struct("@3P3q4i0q")
 _INT8 = struct.Struct("@7PN6qi0q")
-_CODES = {"int8": _lib.DTYPE_INT8, "e4m3": _lib.DTYPE_E4M3}
+
+# A call's host time is its floor at decode sizes, and most of it is spent on
+# asking tensors what they are: each is asked once, and what does not fit is named
+# by the functions below, off the straight path.
+_OUT = {}      # out_dtype, as a name or a torch dtype, and the dtype of the tensor and the library's type for it
+_KIND = {}     # torch dtype of activations: the library's type
+_stream_of = _device_now = None
 
 
-def _run(name, M, packed, index, stream):
-    """The library's call on the given stream, or the current one of the tensors' device, with that device current."""
+def _prepare():
+    """What the calls need of torch, looked up once."""
+    global _stream_of, _device_now
     torch = _torch()
-    if M == 0:
-        return
+    _KIND.update({torch.float32: _lib.DTYPE_F32, torch.bfloat16: _lib.DTYPE_BF16})
+    _OUT.update({"int8": (torch.uint8, _lib.DTYPE_INT8), "e4m3": (torch.uint8, _lib.DTYPE_E4M3)})
+    for name, dt in (("f32", torch.float32), ("bf16", torch.bfloat16)):
+        _OUT[name] = _OUT[dt] = (dt, _KIND[dt])
+    _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _run(name, packed, index, stream):
+    """The library's call on the given stream, or the current one of the tensors' device, with that device current."""
     fn = getattr(_lib._lib or _lib.lib(), name)
-    if torch._C._cuda_getDevice() != index:
-        with torch.cuda.device(index):
-            rc = fn(packed, _stream(stream))
+    if _device_now() != index:
+        with _torch().cuda.device(index):
+            rc = fn(packed, _stream_of(index) if stream is None else stream.cuda_stream)
     else:
-        rc = fn(packed, _stream(stream))
+        rc = fn(packed, _stream_of(index) if stream is None else stream.cuda_stream)
     if rc:
         _lib.check(rc, name)
 
 
-def _rows(t, what, M=None, K=None, index=None):
-    """A [M, K] GPU tensor whose rows are contiguous: its type, row stride and address."""
+def _wrong(t, what, M=None, K=None, dtype=None, index=None):
+    """Raises what is wrong with a tensor that should have rows [M, K] on a GPU."""
     torch = _torch()
-    if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 2:
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{what} must be a two-dimensional tensor")
-    if M is not None and (shape[0] != M or shape[1] != K):
-        raise ValueError(f"{what} must be [{M}, {K}], got {list(shape)}")
-    ld, step = t.stride()
-    if not t.is_cuda or (step != 1 and shape[1] > 1):
+    if M is not None and t.shape != (M, K):
+        raise ValueError(f"{what} must be [{M}, {K}], got {list(t.shape)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{what} must be a CUDA (HIP) tensor with contiguous rows")
     if index is not None and t.get_device() != index:
         raise ValueError(f"{what} is on another device: {t.device}")
-    return ld if shape[0] > 1 else shape[1], t.data_ptr()
-
-
-def _type(t, what):
-    torch = _torch()
-    dt = t.dtype
-    if dt is torch.bfloat16:
-        return _lib.DTYPE_BF16
-    if dt is torch.float32:
-        return _lib.DTYPE_F32
     raise ValueError(f"{what} must be float32 or bfloat16")
 
 
+def _first(t, what):
+    """The tensor that the others go by: its shape, row stride, address and device index."""
+    try:
+        shape = t.shape
+        M, K = shape
+        ld, step = t.stride()
+        index = t.get_device()
+    except (AttributeError, ValueError):
+        _wrong(t, what)
+    if index < 0 or (step != 1 and K > 1):
+        _wrong(t, what)
+    if _stream_of is None:
+        _prepare()
+    return shape, M, K, ld if M > 1 else K, t.data_ptr(), index
+
+
+def _like(t, shape, what, index):
+    """Row stride and address of a tensor of a shape on a device."""
+    try:
+        if t.shape == shape and t.get_device() == index:
+            ld, step = t.stride()
+            if step == 1 or shape[1] == 1:
+                return ld if shape[0] > 1 else shape[1], t.data_ptr()
+    except AttributeError:
+        pass
+    _wrong(t, what, *shape, index=index)
+
+
 def _vec(t, n, what, index):
-    """The address of an fp32 vector of n elements; 0 for None."""
-    if t is None:
-        return 0
+    """The address of an fp32 vector of n elements."""
     torch = _torch()
     try:
-        if t.shape == (n,) and t.dtype is torch.float32 and t.get_device() == index and t.is_contiguous():
+        if t.dtype is torch.float32 and t.shape == (n,) and t.get_device() == index and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
         pass
@@ -76,30 +108,35 @@ def _vec(t, n, what, index):
     raise ValueError(f"{what} is on another device: {t.device}")
 
 
-def _result(out, scales, out_dtype, M, K, default, device, index, stream):
-    """The output of a call: the tensor and its type, and for codes the scales and their address."""
-    torch = _torch()
+def _kind(t, what):
+    try:
+        return _KIND[t.dtype]
+    except KeyError:
+        raise ValueError(f"{what} must be float32 or bfloat16") from None
+
+
+def _result(out, scales, out_dtype, shape, default, like, index, stream):
+    """The output of a call: the tensor, the library's type for it, and for codes the scales and their address."""
     if out_dtype is None:
-        out_dtype = default if out is None or out.dtype is torch.uint8 else out.dtype
-    code = _CODES.get(out_dtype) if isinstance(out_dtype, str) else None
-    if code is None:
-        if isinstance(out_dtype, str):
-            out_dtype = {"f32": torch.float32, "bf16": torch.bfloat16}.get(out_dtype)
-        if out_dtype is not torch.float32 and out_dtype is not torch.bfloat16:
-            raise ValueError("out_dtype must be 'int8', 'e4m3', 'bf16', 'f32' or a torch dtype of the last two")
-        if scales is not None:
-            raise ValueError("scales belong to codes")
-        want, code = out_dtype, _lib.DTYPE_F32 if out_dtype is torch.float32 else _lib.DTYPE_BF16
-    else:
-        want = torch.uint8
+        out_dtype = default if out is None else out.dtype
+    try:
+        want, code = _OUT[out_dtype]
+    except (KeyError, TypeError):
+        raise ValueError("out_dtype must be 'int8', 'e4m3', 'bf16', 'f32' or a torch dtype of the last two") from None
+    if code >= _lib.DTYPE_E4M3:
         if scales is None:
-            scales = _empty((M,), torch.float32, device, stream)
+            scales = _empty(shape[:1], _torch().float32, like.device, stream)
+        at = _vec(scales, shape[0], "scales", index)
+    elif scales is not None:
+        raise ValueError("scales belong to codes")
+    else:
+        at = 0
     if out is None:
-        out = _empty((M, K), want, device, stream)
-    elif out.shape != (M, K) or out.dtype is not want or out.get_device() != index or not out.is_contiguous():
-        _dev(_need(out, (M, K), want, "out"), "out")
+        out = _empty(shape, want, like.device, stream)
+    elif out.dtype is not want or out.shape != shape or out.get_device() != index or not out.is_contiguous():
+        _dev(_need(out, shape, want, "out"), "out")
         raise ValueError(f"out is on another device: {out.device}")
-    return out, code, scales, _vec(scales, M, "scales", index)
+    return out, code, scales, at
 
 
 def block_norm(residual, y=None, weight=None, bias=None, eps: float = 1e-6, layer: bool = False, post_weight=None,
@@ -120,54 +157,57 @@ def block_norm(residual, y=None, weight=None, bias=None, eps: float = 1e-6, laye
     n has out_dtype: 'bf16', 'f32' (default: residual's type), or 'int8' and 'e4m3'
     for uint8 codes and their scales, the Xq and s_a of the products; scales is
     None otherwise.  post_eps defaults to eps."""
-    torch = _torch()
-    ld, at = _rows(residual, "residual")
-    M, K = residual.shape
-    index, device = residual.get_device(), residual.device
-    kind = _type(residual, "residual")
+    shape, M, K, ld, at, index = _first(residual, "residual")
+    kind = _kind(residual, "residual")
     y_at = y_ld = y_kind = to = to_ld = 0
     gate_at = gate_ld = gate_kind = per_row = 0
     if y is not None:
-        y_ld, y_at = _rows(y, "y", M, K, index)
-        y_kind = _type(y, "y")
+        y_ld, y_at = _like(y, shape, "y", index)
+        y_kind = _kind(y, "y")
         if residual_out is None:
-            residual_out = _empty((M, K), residual.dtype, device, stream)
-            to_ld, to = K, residual_out.data_ptr()
-        else:
-            to_ld, to = _rows(residual_out, "residual_out", M, K, index)
-            if residual_out.dtype is not residual.dtype:
-                raise ValueError(f"residual_out must be {residual.dtype}")
+            residual_out = _empty(shape, residual.dtype, residual.device, stream)
+        to_ld, to = _like(residual_out, shape, "residual_out", index)
+        if residual_out.dtype is not residual.dtype:
+            _wrong(residual_out, "residual_out", M, K, residual.dtype)
         if gate is not None:
-            gate_kind, shape = _type(gate, "gate"), gate.shape
-            if gate.get_device() != index:
-                raise ValueError(f"gate is on another device: {gate.device}")
-            gate_at = gate.data_ptr()
-            if shape == (K,) or shape == (1, K):
-                ok = gate.stride(-1) == 1
-            elif shape == (M, K):
-                gate_ld, step = gate.stride()
-                ok, gate_ld = step == 1, gate_ld if M > 1 else 0
-            elif shape == (M, 1):
-                gate_ld, per_row, ok = gate.stride(0) if M > 1 else 0, 1, True
-            else:
-                raise ValueError(f"gate must be [{K}], [1, {K}], [{M}, 1] or [{M}, {K}], got {list(shape)}")
-            if not ok:
-                raise ValueError("the rows of gate must be contiguous")
+            gate_at, gate_ld, gate_kind, per_row = _gate(gate, M, K, index)
     elif gate is not None or post_weight is not None or post_bias is not None or residual_out is not None:
         raise ValueError("gate, post_weight, post_bias and residual_out belong to y")
     if weight is not None:
-        out, code, scales, scales_at = _result(out, scales, out_dtype, M, K, residual.dtype, device, index, stream)
-        out_at = out.data_ptr()
+        out, code, scales, scales_at = _result(out, scales, out_dtype, shape, residual.dtype, residual, index, stream)
+        out_at, weight_at = out.data_ptr(), _vec(weight, K, "weight", index)
     elif y is None or out is not None or bias is not None or scales is not None or out_dtype is not None:
         raise ValueError("out, out_dtype, scales and bias belong to weight, and without y there must be one")
     else:
-        code = scales_at = out_at = 0
-    _run("sdq_block_norm", M, _NORM.pack(
-        at, y_at, gate_at, _vec(weight, K, "weight", index), _vec(bias, K, "bias", index),
-        _vec(post_weight, K, "post_weight", index), _vec(post_bias, K, "post_bias", index), to, out_at, scales_at, M, K, ld, y_ld,
-        gate_ld, to_ld, eps, eps if post_eps is None else post_eps, kind, y_kind, gate_kind, code, per_row, layer, scale),
-        index, stream)
+        code = scales_at = out_at = weight_at = 0
+    if M:
+        _run("sdq_block_norm", _NORM.pack(
+            at, y_at, gate_at, weight_at, 0 if bias is None else _vec(bias, K, "bias", index),
+            0 if post_weight is None else _vec(post_weight, K, "post_weight", index),
+            0 if post_bias is None else _vec(post_bias, K, "post_bias", index), to, out_at, scales_at, M, K, ld, y_ld, gate_ld,
+            to_ld, eps, eps if post_eps is None else post_eps, kind, y_kind, gate_kind, code, per_row, layer, scale), index, stream)
     return residual if y is None else residual_out, out, scales
+
+
+def _gate(gate, M, K, index):
+    """Address, row stride, the library's type of a gate, and whether it is one number per row."""
+    try:
+        shape, stride = gate.shape, gate.stride()
+    except AttributeError:
+        raise ValueError("gate must be a torch tensor") from None
+    kind = _kind(gate, "gate")
+    if gate.get_device() != index:
+        raise ValueError(f"gate is on another device: {gate.device}")
+    ld = per_row = 0
+    if shape == (M, K) and M > 1:
+        ld = stride[0]
+    elif shape == (M, 1):
+        ld, per_row = stride[0] if M > 1 else 0, 1
+    elif shape != (K,) and shape != (1, K):
+        raise ValueError(f"gate must be [{K}], [1, {K}], [{M}, 1] or [{M}, {K}], got {list(shape)}")
+    if not per_row and stride[-1] != 1:
+        raise ValueError("the rows of gate must be contiguous")
+    return gate.data_ptr(), ld, kind, per_row
 
 
 def glu_act(x, act: str = "silu", gated: bool = True, out_dtype=None, out=None, scales=None, stream=None):
@@ -177,19 +217,19 @@ def glu_act(x, act: str = "silu", gated: bool = True, out_dtype=None, out=None, 
     x is [M, 2 F] (gated) or [M, F], fp32 or bf16, as a stacked gate/up projection
     writes it (rows may be strided); act 'silu', 'gelu' (the tanh form) or 'relu';
     out_dtype as in block_norm."""
-    ld, at = _rows(x, "x")
-    M, F = x.shape
+    shape, M, F, ld, at, index = _first(x, "x")
     if gated:
         if F % 2:
             raise ValueError("the rows of x must be two parts of the same width")
         F //= 2
+        shape = (M, F)
     code = _lib.ACT.get(act)
     if code is None:
         raise ValueError("act must be 'silu', 'gelu' or 'relu'")
-    index = x.get_device()
-    kind = _type(x, "x")
-    out, to, scales, scales_at = _result(out, scales, out_dtype, M, F, x.dtype, x.device, index, stream)
-    _run("sdq_glu_act", M, _GLU.pack(at, out.data_ptr(), scales_at, M, F, ld, kind, to, code, gated), index, stream)
+    kind = _kind(x, "x")
+    out, to, scales, scales_at = _result(out, scales, out_dtype, shape, x.dtype, x, index, stream)
+    if M:
+        _run("sdq_glu_act", _GLU.pack(at, out.data_ptr(), scales_at, M, F, ld, kind, to, code, gated), index, stream)
     return out, scales
 
 
@@ -211,21 +251,18 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
     out_dtype (default fp32).  workspace: a uint8 tensor of gemm_int8_workspace_size
     bytes, or a fresh one is made where that is not 0."""
     torch = _torch()
-    x_ld, x_at = _rows(xq, "xq")
-    M, K = xq.shape
-    index = xq.get_device()
-    w_ld, w_at = _rows(wq, "wq", index=index)
-    N = wq.shape[0]
+    _, M, K, x_ld, x_at, index = _first(xq, "xq")
+    _, N, depth, w_ld, w_at, where = _first(wq, "wq")
     for t, what in ((xq, "xq"), (wq, "wq")):
         if t.dtype is not torch.int8 and t.dtype is not torch.uint8:
             raise ValueError(f"{what} must be int8 codes (int8 or uint8)")
-    if wq.shape[1] != K:
-        raise ValueError(f"wq must be [N, {K}], got {list(wq.shape)}")
+    if depth != K or where != index:
+        _wrong(wq, "wq", N, K, index=index)
     if out is None:
         out = _empty((M, N), torch.float32 if out_dtype is None else out_dtype, xq.device, stream)
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise ValueError(f"out must be {out_dtype}")
-    y_ld, y_at = _rows(out, "out", M, N, index)
+    y_ld, y_at = _like(out, (M, N), "out", index)
     need = gemm_int8_workspace_size(M, N, K)
     ws = ws_bytes = 0
     if need:
@@ -234,7 +271,9 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
         elif _need_bytes(workspace, need, "workspace").get_device() != index:
             raise ValueError(f"workspace is on another device: {workspace.device}")
         ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    _run("sdq_gemm_int8", M, _INT8.pack(
-        x_at, w_at, _vec(s_x, M, "s_x", index), _vec(s_w, N, "s_w", index), _vec(bias, N, "bias", index), y_at, ws, ws_bytes, M, N, K, x_ld, w_ld,
-        y_ld, _type(out, "out")), index, stream)
+    packed = _INT8.pack(
+        x_at, w_at, _vec(s_x, M, "s_x", index), _vec(s_w, N, "s_w", index), 0 if bias is None else _vec(bias, N, "bias", index), y_at,
+        ws, ws_bytes, M, N, K, x_ld, w_ld, y_ld, _kind(out, "out"))
+    if M:
+        _run("sdq_gemm_int8", packed, index, stream)
     return out
