@@ -81,6 +81,7 @@ extern "C" sdq_status sdq_block_norm(const sdq_norm_args* t, void* stream) {
   a.residual_out_stride = t->residual_out_stride;
   a.eps = t->eps;
   a.post_eps = t->post_eps;
+  a.per = 1.0 / double(K);
   a.M = uint32_t(M);
   a.K = uint32_t(K);
   a.x_type = t->residual_dtype;

@@ -16,7 +16,7 @@ struct NormArgs {
   void *residual_out, *out;
   float* scales;
   int64_t residual_stride, y_stride, gate_stride, residual_out_stride;  // elements
-  double eps, post_eps;
+  double eps, post_eps, per;  // per: 1 / K
   uint32_t M, K;
   int x_type, y_type, gate_type, out_type;  // residual's, y's (or kNone), ...
   bool gate_cols;                           // one gate for each element of a row, not one for the row

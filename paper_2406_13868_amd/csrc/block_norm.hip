@@ -36,32 +36,36 @@ struct Row {
       gate_of_row = a.gate_type == kF32 ? static_cast<const float*>(a.gate)[m * a.gate_stride]
                                         : __uint_as_float(uint32_t(static_cast<const uint16_t*>(a.gate)[m * a.gate_stride]) << 16);
   }
-  // r += (u * gate) * scale for the eight elements from k
-  __device__ __forceinline__ void join(int64_t k, const float (&u)[8], float (&r)[8]) const {
-    float g[8];
+  // r += (u * gate) * scale for the eight elements from k; a product by one changes nothing
+  __device__ __forceinline__ void join(int64_t k, float (&u)[8], float (&r)[8]) const {
     if (a.gate && a.gate_cols) {
+      float g[8];
       load8(a.gate_type, a.gate, m * a.gate_stride + k, g);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = gate_of_row;
+      for (int i = 0; i < 8; ++i) u[i] = u[i] * g[i];
+    } else if (a.gate) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = u[i] * gate_of_row;
+    }
+    if (a.scale != 1.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = u[i] * a.scale;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = u[i] * g[i];
-      r[i] = r[i] + t * a.scale;
-    }
+    for (int i = 0; i < 8; ++i) r[i] = r[i] + u[i];
   }
 };
 
 // v = d * rstd * w + b for the eight elements from k, d = v - mean
-__device__ __forceinline__ void apply(float (&v)[8], double mean, float rstd, const float* w, const float* b, int64_t k) {
+__device__ __forceinline__ void apply(float (&v)[8], bool layer, double mean, float rstd, const float* w, const float* b, int64_t k) {
   float g[8];
   load8<true>(w, k, g);
+  if (layer) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float d = float(double(v[i]) - mean);
-    v[i] = d * rstd * g[i];
+    for (int i = 0; i < 8; ++i) v[i] = float(double(v[i]) - mean);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * g[i];
   if (b) {
     load8<true>(b, k, g);
 #pragma unroll
@@ -69,96 +73,189 @@ __device__ __forceinline__ void apply(float (&v)[8], double mean, float rstd, co
   }
 }
 
-__device__ __forceinline__ float root(double sum, uint32_t K, double eps) { return float(1.0 / sqrt(sum / double(K) + eps)); }
+// 1 / sqrt(sum / K + eps): the reciprocal root instruction is 2^-24 off or better,
+// two steps of Newton's leave fp64's own roundings.  (The division and the root that
+// the compiler makes are 150 instructions for every thread.)
+__device__ __forceinline__ float root(double sum, double per, double eps) {
+  const double x = __builtin_fma(sum, per, eps);
+  double y = __builtin_amdgcn_rsq(x);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+  return x == __builtin_huge_val() ? 0.f : float(y);
+}
 
-template <int NT, int CH>
-struct Held {
-  float v[CH][8];
-};
 
-// Mean (layer only) and reciprocal root of a held row.
+// Mean (layer only) and reciprocal root of a held row, whose places past its end are 0.
 template <int NT, int CH>
 __device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint32_t P, const NormArgs& a, double eps, double* red,
                                       double& mean, float& rstd) {
   mean = 0.0;
+  double s = 0.0;
   if (a.layer) {
-    double s = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += double(v[c][i]);  // 0 past the row
-    mean = row_sum<NT>(s, red) / double(a.K);
-  }
-  double s = 0.0;
+      for (int i = 0; i < 8; ++i) s += double(v[c][i]);
+    mean = row_sum<NT>(s, red) * a.per;
+    s = 0.0;
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (t + c * NT < P)
+    for (int c = 0; c < CH; ++c) {
+      const double mu = t + c * NT < P ? mean : 0.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const double d = double(v[c][i]) - mean;
+        const double d = double(v[c][i]) - mu;
         s = __builtin_fma(d, d, s);
       }
-  rstd = root(row_sum<NT>(s, red + NT / 64), a.K, eps);
-}
-
-template <bool XF32, int NT, int CH>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArgs a) {
-  __shared__ double red[4 * (NT / 64)];
-  __shared__ uint32_t top[NT / 64];
-  const uint32_t t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, P = a.K / 8;
-  const int64_t m = NT == 64 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
-  if (m >= a.M) return;  // whole waves, and none that others wait for
-  const Row row(a, m);
-  float r[CH][8] = {};
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (t + c * NT < P) load8<XF32>(a.residual, m * a.residual_stride + (t + c * NT) * 8, r[c]);
-  if (a.y_type != kNone) {
-    float u[CH][8] = {};
+    }
+  } else {
 #pragma unroll
     for (int c = 0; c < CH; ++c)
-      if (t + c * NT < P) load8(a.y_type, a.y, m * a.y_stride + (t + c * NT) * 8, u[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = __builtin_fma(double(v[c][i]), double(v[c][i]), s);
+  }
+  rstd = root(row_sum<NT>(s, red + NT / 64), a.per, eps);
+}
+
+// A held row's weights (and biases), on their way while something else is done.
+template <int CH>
+struct Weights {
+  Raw8<true> w[CH], b[CH];
+  __device__ __forceinline__ void load(const float* weight, const float* bias, uint32_t K, uint32_t t, int nt) {
+    const RowBuf<true> wr(weight, 0, K);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c].load(wr, t + c * nt);
+    if (bias) {
+      const RowBuf<true> br(bias, 0, K);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) b[c].load(br, t + c * nt);
+    }
+  }
+  // v = d * rstd * w + b, d = v - mean
+  __device__ __forceinline__ void apply(float (&v)[CH][8], bool layer, double mean, float rstd, bool bias) const {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float g[8];
+      w[c].widen(g);
+      if (layer) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mean);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * g[i];
+      if (bias) {
+        b[c].widen(g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] + g[i];
+      }
+    }
+  }
+};
+
+// YT: y's type, or kNone.
+template <bool XF32, int YT, int NT, int CH>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArgs a) {
+  constexpr bool YF32 = YT == kF32;
+  __shared__ double red[4 * (NT / 64)];
+  __shared__ uint32_t top[NT / 64];
+  const uint32_t t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, P = a.K / 8, K = a.K;
+  const int64_t m = NT == 64 ? int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int64_t(blockIdx.x);
+  if (m >= a.M) return;  // whole waves, and none that others wait for
+  const RowBuf<XF32> xr(a.residual, m * a.residual_stride, K);
+  Raw8<XF32> x[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) x[c].load(xr, t + c * NT);
+  float r[CH][8];
+  Weights<CH> w;
+  if constexpr (YT != kNone) {
+    const RowBuf<YF32> yr(a.y, m * a.y_stride, K);
+    Raw8<YF32> y[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) y[c].load(yr, t + c * NT);
+    if (a.post_weight) w.load(a.post_weight, a.post_bias, K, t, NT);
+    // a gate of y's own type, as a rule: of the other it is asked for when it is used
+    const bool cols = a.gate && a.gate_cols, ready = cols && (a.gate_type == kF32) == YF32;
+    Raw8<YF32> g[CH];
+    if (ready) {
+      const RowBuf<YF32> gr(a.gate, m * a.gate_stride, K);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) g[c].load(gr, t + c * NT);
+    }
+    const Row row(a, m);
+    float u[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) y[c].widen(u[c]);
     if (a.post_weight) {
       double mean;
       float rstd;
       stats<NT, CH>(u, t, P, a, a.post_eps, red, mean, rstd);
+      w.apply(u, a.layer, mean, rstd, a.post_bias != nullptr);
+    }
+    if (a.weight) w.load(a.weight, a.bias, K, t, NT);
+    if (cols) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        float f[8];
+        if (ready) {
+          g[c].widen(f);
+        } else {
+          Raw8<!YF32> other;
+          other.load(RowBuf<!YF32>(a.gate, m * a.gate_stride, K), t + c * NT);
+          other.widen(f);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * f[i];
+      }
+    } else if (a.gate) {
 #pragma unroll
       for (int c = 0; c < CH; ++c)
-        if (t + c * NT < P) apply(u[c], mean, rstd, a.post_weight, a.post_bias, (t + c * NT) * 8);
-    }
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-      if (t + c * NT < P) {
-        row.join((t + c * NT) * 8, u[c], r[c]);
-        store8(XF32, a.residual_out, m * a.residual_out_stride + (t + c * NT) * 8, r[c]);
-      }
+        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * row.gate_of_row;
+    }
+    if (a.scale != 1.f) {  // a product by one changes nothing
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * a.scale;
+    }
+    const RowBuf<XF32> to(a.residual_out, m * a.residual_out_stride, K);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      x[c].widen(r[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[c][i] = r[c][i] + u[c][i];
+      store8(to, t + c * NT, r[c]);
+    }
+  } else {
+    w.load(a.weight, a.bias, K, t, NT);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) x[c].widen(r[c]);
   }
   if (!a.weight) return;
   double mean;
   float rstd;
   stats<NT, CH>(r, t, P, a, a.eps, red + 2 * (NT / 64), mean, rstd);
-  uint32_t most = 0;
+  w.apply(r, a.layer, mean, rstd, a.bias != nullptr);
+  const int64_t to = m * K;
+  if (a.out_type == kF32) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (t + c * NT < P) {
-      apply(r[c], mean, rstd, a.weight, a.bias, (t + c * NT) * 8);
+    for (int c = 0; c < CH; ++c) store8(RowBuf<true>(a.out, to, K), t + c * NT, r[c]);
+  } else if (a.out_type == kBF16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most = max(most, abs_bits(r[c][i]));
-    }
-  const int64_t to = m * a.K;
-  if (a.out_type == kF32 || a.out_type == kBF16) {
+    for (int c = 0; c < CH; ++c) store8(RowBuf<false>(a.out, to, K), t + c * NT, r[c]);
+  } else {
+    float most = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
-      if (t + c * NT < P) store8(a.out_type == kF32, a.out, to + (t + c * NT) * 8, r[c]);
-    return;
-  }
-  const bool e4m3 = a.out_type == kE4M3;
-  const RowCode code(row_umax<NT>(most, top), e4m3);
-  if (t == 0) a.scales[m] = code.s;
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (t + c * NT < P)
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + to + (t + c * NT) * 8) = codes8(r[c], code, e4m3);
+      for (int i = 0; i < 8; ++i) most = abs_max(most, r[c][i]);
+    const bool e4m3 = a.out_type == kE4M3;
+    const RowCode code(row_umax<NT>(abs_bits(most), top), e4m3);
+    if (t == 0) a.scales[m] = code.scale();
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (t + c * NT < P)
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + to + (t + c * NT) * 8) = codes8(r[c], code, e4m3);
+  }
 }
 
 // Rows of any width: each sum reads the row again.  The stream is written in the
@@ -177,7 +274,7 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
     if (a.y_type == kNone) return;
     float u[8];
     block_out(k, u);
-    if (a.post_weight) apply(u, post_mean, post_rstd, a.post_weight, a.post_bias, k);
+    if (a.post_weight) apply(u, a.layer, post_mean, post_rstd, a.post_weight, a.post_bias, k);
     row.join(k, u, r);
   };
   auto sums = [&](auto&& values, double eps, double* red0, double* red1, double& mu, float& root_of) {
@@ -189,7 +286,7 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += double(v[i]);
       }
-      mu = row_sum<NT>(s, red0) / double(a.K);
+      mu = row_sum<NT>(s, red0) * a.per;
     }
     double s = 0.0;
     for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
@@ -201,40 +298,46 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
         s = __builtin_fma(d, d, s);
       }
     }
-    root_of = root(row_sum<NT>(s, red1), a.K, eps);
+    root_of = root(row_sum<NT>(s, red1), a.per, eps);
   };
   if (a.y_type != kNone && a.post_weight) sums(block_out, a.post_eps, red[0], red[1], post_mean, post_rstd);
   const bool coded = a.weight && (a.out_type == kInt8 || a.out_type == kE4M3), e4m3 = a.out_type == kE4M3;
-  uint32_t most = 0;
+  float most = 0.f;
   if (a.weight) {
     sums(stream, a.eps, red[2], red[3], mean, rstd);
     if (coded)
       for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
         float v[8];
         stream(k, v);
-        apply(v, mean, rstd, a.weight, a.bias, k);
+        apply(v, a.layer, mean, rstd, a.weight, a.bias, k);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(v[i]));
+        for (int i = 0; i < 8; ++i) most = abs_max(most, v[i]);
       }
   }
-  const RowCode code(coded ? row_umax<NT>(most, top) : 0u, e4m3);
-  if (coded && threadIdx.x == 0) a.scales[m] = code.s;
+  const RowCode code(coded ? row_umax<NT>(abs_bits(most), top) : 0u, e4m3);
+  if (coded && threadIdx.x == 0) a.scales[m] = code.scale();
   for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {
     float v[8];
     stream(k, v);
     if (a.y_type != kNone) store8(a.x_type == kF32, a.residual_out, m * a.residual_out_stride + k, v);
     if (!a.weight) continue;
-    apply(v, mean, rstd, a.weight, a.bias, k);
+    apply(v, a.layer, mean, rstd, a.weight, a.bias, k);
     if (coded) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + m * K + k) = codes8(v, code, e4m3);
     else store8(a.out_type == kF32, a.out, m * K + k, v);
   }
 }
 
-template <int NT, int CH>
+template <bool XF32, int NT, int CH>
 void launch(const NormArgs& a, hipStream_t st) {
   const dim3 grid(NT == 64 ? (a.M + 3) / 4 : a.M), block(NT == 64 ? 256 : NT);
-  if (a.x_type == kF32) hipLaunchKernelGGL((block_norm_kernel<true, NT, CH>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((block_norm_kernel<false, NT, CH>), grid, block, 0, st, a);
+  if (a.y_type == kF32) hipLaunchKernelGGL((block_norm_kernel<XF32, kF32, NT, CH>), grid, block, 0, st, a);
+  else if (a.y_type == kBF16) hipLaunchKernelGGL((block_norm_kernel<XF32, kBF16, NT, CH>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((block_norm_kernel<XF32, kNone, NT, CH>), grid, block, 0, st, a);
+}
+template <int NT, int CH>
+void launch(const NormArgs& a, hipStream_t st) {
+  if (a.x_type == kF32) launch<true, NT, CH>(a, st);
+  else launch<false, NT, CH>(a, st);
 }
 
 }  // namespace

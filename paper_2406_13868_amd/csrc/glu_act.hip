@@ -9,6 +9,8 @@
 // differ in an fp32's last bit would give other codes now and then.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "row_ops.h"
 #include "sdq.h"
 
@@ -19,57 +21,80 @@ namespace {
 
 constexpr uint32_t kMostHeld = 32768;
 
-// exp(t) within 1e-14 of itself for |t| <= 700: t = n ln 2 + r with |r| <= ln 2 / 2,
-// exp(r) by its series up to r^11 / 11! (the next term is 6e-15), times 2^n.
+// exp(t) within 2e-14 of itself for |t| <= 700: t = n ln 2 + r with |r| <= ln 2 / 2,
+// exp(r) by the polynomial of degree 9 that meets it at the ten Chebyshev nodes of
+// that range (1.9e-14 off at most), times 2^n, whose n is the low word of
+// t / ln 2 + 1.5 * 2^52.
 __device__ __forceinline__ double exp64(double t) {
-  const double n = __builtin_rint(t * 1.4426950408889634);
-  double r = __builtin_fma(n, -0.6931471805599453, t);
-  r = __builtin_fma(n, -2.3190468138462996e-17, r);  // ln 2 less its fp64
-  double p = 1.0 / 39916800;
-  p = __builtin_fma(p, r, 1.0 / 3628800);
-  p = __builtin_fma(p, r, 1.0 / 362880);
-  p = __builtin_fma(p, r, 1.0 / 40320);
-  p = __builtin_fma(p, r, 1.0 / 5040);
-  p = __builtin_fma(p, r, 1.0 / 720);
-  p = __builtin_fma(p, r, 1.0 / 120);
-  p = __builtin_fma(p, r, 1.0 / 24);
-  p = __builtin_fma(p, r, 1.0 / 6);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  return __builtin_ldexp(p, int(n));
+  const double shifted = __builtin_fma(t, 1.4426950408889634, 0x1.8p52);
+  const double r = __builtin_fma(shifted - 0x1.8p52, -0.6931471805599453, t);
+  double p = 2.7632640675430236e-06;
+  p = __builtin_fma(p, r, 2.4884459751751116e-05);
+  p = __builtin_fma(p, r, 0.0001984119064754424);
+  p = __builtin_fma(p, r, 0.0013888801749656543);
+  p = __builtin_fma(p, r, 0.008333333367311603);
+  p = __builtin_fma(p, r, 0.04166666704055191);
+  p = __builtin_fma(p, r, 0.16666666666615648);
+  p = __builtin_fma(p, r, 0.4999999999943859);
+  p = __builtin_fma(p, r, 1.0000000000000013);
+  p = __builtin_fma(p, r, 1.0000000000000135);
+  const uint64_t bits = __builtin_bit_cast(uint64_t, p), n = __builtin_bit_cast(uint64_t, shifted);
+  return __builtin_bit_cast(double, uint64_t(uint32_t(bits >> 32) + (uint32_t(n) << 20)) << 32 | uint32_t(bits));
 }
 
-// g / (1 + exp(t)).  t is held to where exp is finite: at the upper end the
+// g / (1 + exp(t)): the reciprocal instruction is 2^-24 off, after a step of
+// Newton's 2^-48.  HELD: t is held to where exp is finite; at the upper end the
 // quotient is below fp32's least number, at the lower it is g.
+template <bool HELD>
 __device__ __forceinline__ double gate64(double g, double t) {
-  t = fmin(fmax(t, -700.0), 700.0);
+  if constexpr (HELD) t = fmin(fmax(t, -700.0), 700.0);
   const double q = 1.0 + exp64(t);
-  double x = __builtin_amdgcn_rcp(q);
-  x = __builtin_fma(x, __builtin_fma(-q, x, 1.0), x);  // Newton's steps for 1 / q
-  x = __builtin_fma(x, __builtin_fma(-q, x, 1.0), x);
-  return g * x;
+  const double x = __builtin_amdgcn_rcp(q);
+  return g * __builtin_fma(x, __builtin_fma(-q, x, 1.0), x);
 }
 
+// Up to this magnitude of g, t stays where exp is finite.
 template <int ACT>
+constexpr float kFree = ACT == SDQ_ACT_SILU ? 700.f : 20.f;
+template <int ACT, bool HELD>
 __device__ __forceinline__ double act64(double g) {
-  if constexpr (ACT == SDQ_ACT_SILU) return gate64(g, -g);
-  if constexpr (ACT == SDQ_ACT_GELU) return gate64(g, -1.5957691216057308 * (g + 0.044715 * (g * g * g)));
-  return g > 0.0 || g != g ? g : 0.0;
+  if constexpr (ACT == SDQ_ACT_SILU) return gate64<HELD>(g, -g);
+  return gate64<HELD>(g, -1.5957691216057308 * (g + 0.044715 * (g * g * g)));
+}
+
+// h of eight elements
+template <int ACT, bool GATED>
+__device__ __forceinline__ void activate(const float (&g)[8], const float (&u)[8], float (&h)[8]) {
+  if constexpr (ACT == SDQ_ACT_RELU) {  // one product of fp32 numbers: rounded once in fp32 too
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      h[i] = g[i] > 0.f || g[i] != g[i] ? g[i] : 0.f;
+      if constexpr (GATED) h[i] = h[i] * u[i];
+    }
+    return;
+  }
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = abs_max(most, g[i]);
+  const auto all = [&](auto held) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      double v = act64<ACT, decltype(held)::value>(double(g[i]));
+      if constexpr (GATED) v = v * double(u[i]);
+      h[i] = float(v);
+    }
+  };
+  if (__any(!(most <= kFree<ACT>))) all(std::true_type());  // NaN too
+  else all(std::false_type());
 }
 
 // h of the eight elements from k of a row
 template <int ACT, bool XF32, bool GATED>
 __device__ __forceinline__ void values(const GluArgs& a, int64_t row, int64_t k, float (&h)[8]) {
-  float g[8], u[8];
+  float g[8], u[8] = {};
   load8<XF32>(a.x, row + k, g);
   if constexpr (GATED) load8<XF32>(a.x, row + a.F + k, u);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    double v = act64<ACT>(double(g[i]));
-    if constexpr (GATED) v = v * double(u[i]);
-    h[i] = float(v);
-  }
+  activate<ACT, GATED>(g, u, h);
 }
 
 template <int ACT, bool XF32, bool GATED, int NT, int CH>
@@ -78,17 +103,30 @@ __global__ __launch_bounds__(NT) void glu_code_kernel(GluArgs a) {
   const uint32_t t = threadIdx.x, P = a.F / 8;
   const int64_t m = blockIdx.x, from = m * a.x_stride;
   const bool e4m3 = a.out_type == kE4M3;
-  float h[CH][8] = {};
-  uint32_t most = 0;
+  const RowBuf<XF32> gr(a.x, from, a.F), ur(a.x, GATED ? from + a.F : from, a.F);
+  Raw8<XF32> gq[CH], uq[CH];
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (t + c * NT < P) {
-      values<ACT, XF32, GATED>(a, from, (t + c * NT) * 8, h[c]);
+  for (int c = 0; c < CH; ++c) {
+    gq[c].load(gr, t + c * NT);
+    if constexpr (GATED) uq[c].load(ur, t + c * NT);
+  }
+  float h[CH][8], most = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most = max(most, abs_bits(h[c][i]));
+  for (int c = 0; c < CH; ++c) {
+    if (c > 0 && __builtin_amdgcn_readfirstlane(t) + c * NT >= P) {  // the whole wave is past the row
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[c][i] = 0.f;
+      continue;
     }
-  const RowCode code(row_umax<NT>(most, top), e4m3);
-  if (t == 0) a.scales[m] = code.s;
+    float g[8], u[8] = {};
+    gq[c].widen(g);
+    if constexpr (GATED) uq[c].widen(u);
+    activate<ACT, GATED>(g, u, h[c]);  // 0 past the row
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = abs_max(most, h[c][i]);
+  }
+  const RowCode code(row_umax<NT>(abs_bits(most), top), e4m3);
+  if (t == 0) a.scales[m] = code.scale();
 #pragma unroll
   for (int c = 0; c < CH; ++c)
     if (t + c * NT < P)
@@ -103,15 +141,15 @@ __global__ __launch_bounds__(1024) void glu_code_wide(GluArgs a) {
   __shared__ uint32_t top[NT / 64];
   const int64_t m = blockIdx.x, from = m * a.x_stride;
   const bool e4m3 = a.out_type == kE4M3;
-  uint32_t most = 0;
+  float most = 0.f;
   for (int64_t k = threadIdx.x * 8; k < a.F; k += NT * 8) {
     float h[8];
     values<ACT, XF32, GATED>(a, from, k, h);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, abs_bits(h[i]));
+    for (int i = 0; i < 8; ++i) most = abs_max(most, h[i]);
   }
-  const RowCode code(row_umax<NT>(most, top), e4m3);
-  if (threadIdx.x == 0) a.scales[m] = code.s;
+  const RowCode code(row_umax<NT>(abs_bits(most), top), e4m3);
+  if (threadIdx.x == 0) a.scales[m] = code.scale();
   for (int64_t k = threadIdx.x * 8; k < a.F; k += NT * 8) {
     float h[8];
     values<ACT, XF32, GATED>(a, from, k, h);
