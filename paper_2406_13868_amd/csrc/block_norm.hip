@@ -16,6 +16,8 @@
 // read again for each sum instead.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "row_ops.h"
 
 #pragma clang fp contract(off)
@@ -23,7 +25,7 @@
 namespace sdq {
 namespace {
 
-constexpr uint32_t kMostHeld = 32768;
+constexpr uint32_t kMostHeld = 16384;
 
 // What a row needs of the arguments, its pointers' types decided at run time:
 // the branches are uniform.
@@ -86,17 +88,17 @@ __device__ __forceinline__ float root(double sum, double per, double eps) {
 
 
 // Mean (layer only) and reciprocal root of a held row, whose places past its end are 0.
-template <int NT, int CH>
-__device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint32_t P, const NormArgs& a, double eps, double* red,
-                                      double& mean, float& rstd) {
+template <bool LAYER, int NT, int CH>
+__device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint32_t P, double per, double eps, double* red, double& mean,
+                                      float& rstd) {
   mean = 0.0;
   double s = 0.0;
-  if (a.layer) {
+  if constexpr (LAYER) {
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += double(v[c][i]);
-    mean = row_sum<NT>(s, red) * a.per;
+    mean = row_sum<NT>(s, red) * per;
     s = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -113,148 +115,165 @@ __device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint3
 #pragma unroll
       for (int i = 0; i < 8; ++i) s = __builtin_fma(double(v[c][i]), double(v[c][i]), s);
   }
-  rstd = root(row_sum<NT>(s, red + NT / 64), a.per, eps);
+  rstd = root(row_sum<NT>(s, red + NT / 64), per, eps);
 }
 
-// A held row's weights (and biases), on their way while something else is done.
-template <int CH>
+// The weights (and biases) of a thread's pieces.
+template <bool LAYER, int CH>
 struct Weights {
-  Raw8<true> w[CH], b[CH];
+  Raw8<true> w[CH], b[LAYER ? CH : 1];
   __device__ __forceinline__ void load(const float* weight, const float* bias, uint32_t K, uint32_t t, int nt) {
     const RowBuf<true> wr(weight, 0, K);
 #pragma unroll
     for (int c = 0; c < CH; ++c) w[c].load(wr, t + c * nt);
-    if (bias) {
-      const RowBuf<true> br(bias, 0, K);
+    if constexpr (LAYER)
+      if (bias) {
+        const RowBuf<true> br(bias, 0, K);
 #pragma unroll
-      for (int c = 0; c < CH; ++c) b[c].load(br, t + c * nt);
-    }
+        for (int c = 0; c < CH; ++c) b[c].load(br, t + c * nt);
+      }
   }
   // v = d * rstd * w + b, d = v - mean
-  __device__ __forceinline__ void apply(float (&v)[CH][8], bool layer, double mean, float rstd, bool bias) const {
+  __device__ __forceinline__ void apply(float (&v)[CH][8], double mean, float rstd, bool bias) const {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float g[8];
       w[c].widen(g);
-      if (layer) {
+      if constexpr (LAYER) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mean);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * g[i];
-      if (bias) {
-        b[c].widen(g);
+      if constexpr (LAYER)
+        if (bias) {
+          b[c].widen(g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] + g[i];
-      }
+          for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] + g[i];
+        }
     }
   }
 };
 
-// YT: y's type, or kNone.
-template <bool XF32, int YT, int NT, int CH>
+// YT: y's type, or kNone.  NT threads a row, in pieces of eight elements, CH each; a
+// wave's rows are four to a workgroup.  A workgroup takes rows one after the other:
+// what all rows share (weights, a row of gates) is loaded once, and the next row is on
+// its way while one is worked on.
+template <bool XF32, int YT, bool LAYER, int NT, int CH>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArgs a) {
-  constexpr bool YF32 = YT == kF32;
-  __shared__ double red[4 * (NT / 64)];
-  __shared__ uint32_t top[NT / 64];
+  constexpr bool YF32 = YT == kF32, kAhead = CH <= 2;  // more pieces leave no registers for a second row
+  constexpr uint32_t kRows = NT == 64 ? 4 : 1;
+  __shared__ double red[2][4 * (NT / 64)];
+  __shared__ uint32_t top[2][NT / 64];
   const uint32_t t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, P = a.K / 8, K = a.K;
-  const int64_t m = NT == 64 ? int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int64_t(blockIdx.x);
+  uint32_t m = NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
   if (m >= a.M) return;  // whole waves, and none that others wait for
-  const RowBuf<XF32> xr(a.residual, m * a.residual_stride, K);
   Raw8<XF32> x[CH];
+  Raw8<YF32> y[CH], g[CH];
+  const auto request = [&](uint32_t row) {
+    const RowBuf<XF32> xr(a.residual, int64_t(row) * a.residual_stride, K);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) x[c].load(xr, t + c * NT);
-  float r[CH][8];
-  Weights<CH> w;
-  if constexpr (YT != kNone) {
-    const RowBuf<YF32> yr(a.y, m * a.y_stride, K);
-    Raw8<YF32> y[CH];
+    for (int c = 0; c < CH; ++c) x[c].load(xr, t + c * NT);
+    if constexpr (YT != kNone) {
+      const RowBuf<YF32> yr(a.y, int64_t(row) * a.y_stride, K);
 #pragma unroll
-    for (int c = 0; c < CH; ++c) y[c].load(yr, t + c * NT);
-    if (a.post_weight) w.load(a.post_weight, a.post_bias, K, t, NT);
-    // a gate of y's own type, as a rule: of the other it is asked for when it is used
-    const bool cols = a.gate && a.gate_cols, ready = cols && (a.gate_type == kF32) == YF32;
-    Raw8<YF32> g[CH];
-    if (ready) {
-      const RowBuf<YF32> gr(a.gate, m * a.gate_stride, K);
-#pragma unroll
-      for (int c = 0; c < CH; ++c) g[c].load(gr, t + c * NT);
+      for (int c = 0; c < CH; ++c) y[c].load(yr, t + c * NT);
     }
-    const Row row(a, m);
-    float u[CH][8];
+  };
+  // a gate of y's own type, as a rule: of the other it is asked for when it is used
+  const bool cols = YT != kNone && a.gate && a.gate_cols, ready = cols && (a.gate_type == kF32) == YF32;
+  const auto request_gate = [&](uint32_t row) {
+    const RowBuf<YF32> gr(a.gate, int64_t(row) * a.gate_stride, K);
 #pragma unroll
-    for (int c = 0; c < CH; ++c) y[c].widen(u[c]);
-    if (a.post_weight) {
-      double mean;
-      float rstd;
-      stats<NT, CH>(u, t, P, a, a.post_eps, red, mean, rstd);
-      w.apply(u, a.layer, mean, rstd, a.post_bias != nullptr);
-    }
-    if (a.weight) w.load(a.weight, a.bias, K, t, NT);
-    if (cols) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        float f[8];
-        if (ready) {
-          g[c].widen(f);
-        } else {
-          Raw8<!YF32> other;
-          other.load(RowBuf<!YF32>(a.gate, m * a.gate_stride, K), t + c * NT);
-          other.widen(f);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * f[i];
-      }
-    } else if (a.gate) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * row.gate_of_row;
-    }
-    if (a.scale != 1.f) {  // a product by one changes nothing
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * a.scale;
-    }
-    const RowBuf<XF32> to(a.residual_out, m * a.residual_out_stride, K);
+    for (int c = 0; c < CH; ++c) g[c].load(gr, t + c * NT);
+  };
+  request(m);
+  Weights<LAYER, CH> w, pw;
+  if (YT != kNone && a.post_weight) pw.load(a.post_weight, a.post_bias, K, t, NT);
+  if (ready) request_gate(m);
+  if (a.weight) w.load(a.weight, a.bias, K, t, NT);
+  for (uint32_t turn = 0;; turn ^= 1) {
+    float r[CH][8], u[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       x[c].widen(r[c]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[c][i] = r[c][i] + u[c][i];
-      store8(to, t + c * NT, r[c]);
+      if constexpr (YT != kNone) y[c].widen(u[c]);
     }
-  } else {
-    w.load(a.weight, a.bias, K, t, NT);
+    const uint32_t next = m + gridDim.x * kRows;
+    if (kAhead && next < a.M) request(next);
+    if constexpr (YT != kNone) {
+      const Row row(a, m);
+      if (a.post_weight) {
+        double mean;
+        float rstd;
+        stats<LAYER, NT, CH>(u, t, P, a.per, a.post_eps, red[turn], mean, rstd);
+        pw.apply(u, mean, rstd, a.post_bias != nullptr);
+      }
+      if (cols) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) x[c].widen(r[c]);
-  }
-  if (!a.weight) return;
-  double mean;
-  float rstd;
-  stats<NT, CH>(r, t, P, a, a.eps, red + 2 * (NT / 64), mean, rstd);
-  w.apply(r, a.layer, mean, rstd, a.bias != nullptr);
-  const int64_t to = m * K;
-  if (a.out_type == kF32) {
+        for (int c = 0; c < CH; ++c) {
+          float f[8];
+          if (ready) {
+            g[c].widen(f);
+          } else {
+            Raw8<!YF32> other;
+            other.load(RowBuf<!YF32>(a.gate, int64_t(m) * a.gate_stride, K), t + c * NT);
+            other.widen(f);
+          }
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store8(RowBuf<true>(a.out, to, K), t + c * NT, r[c]);
-  } else if (a.out_type == kBF16) {
+          for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * f[i];
+        }
+        if (ready && a.gate_stride && next < a.M) request_gate(next);
+      } else if (a.gate) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store8(RowBuf<false>(a.out, to, K), t + c * NT, r[c]);
-  } else {
-    float most = 0.f;
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+          for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * row.gate_of_row;
+      }
+      if (a.scale != 1.f) {  // a product by one changes nothing
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most = abs_max(most, r[c][i]);
-    const bool e4m3 = a.out_type == kE4M3;
-    const RowCode code(row_umax<NT>(abs_bits(most), top), e4m3);
-    if (t == 0) a.scales[m] = code.scale();
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-      if (t + c * NT < P)
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + to + (t + c * NT) * 8) = codes8(r[c], code, e4m3);
+          for (int i = 0; i < 8; ++i) u[c][i] = u[c][i] * a.scale;
+      }
+      const RowBuf<XF32> to(a.residual_out, int64_t(m) * a.residual_out_stride, K);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[c][i] = r[c][i] + u[c][i];
+        store8(to, t + c * NT, r[c]);
+      }
+    }
+    if (a.weight) {
+      double mean;
+      float rstd;
+      stats<LAYER, NT, CH>(r, t, P, a.per, a.eps, red[turn] + 2 * (NT / 64), mean, rstd);
+      w.apply(r, mean, rstd, a.bias != nullptr);
+      const int64_t to = int64_t(m) * K;
+      if (a.out_type == kF32) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) store8(RowBuf<true>(a.out, to, K), t + c * NT, r[c]);
+      } else if (a.out_type == kBF16) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) store8(RowBuf<false>(a.out, to, K), t + c * NT, r[c]);
+      } else {
+        float most = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) most = abs_max(most, r[c][i]);
+        const bool e4m3 = a.out_type == kE4M3;
+        const RowCode code(row_umax<NT>(abs_bits(most), top[turn]), e4m3);
+        if (t == 0) a.scales[m] = code.scale();
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+          if (t + c * NT < P)
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + to + (t + c * NT) * 8) = codes8(r[c], code, e4m3);
+      }
+    }
+    if (next >= a.M) break;
+    m = next;
+    if (!kAhead) request(m);
   }
 }
 
@@ -327,30 +346,40 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
   }
 }
 
-template <bool XF32, int NT, int CH>
+// Workgroups of 256 compute units' worth of waves, each taking rows in turn.
+constexpr uint32_t kWaves = 256 * 16;
+
+template <bool XF32, int YT, int NT, int CH>
 void launch(const NormArgs& a, hipStream_t st) {
-  const dim3 grid(NT == 64 ? (a.M + 3) / 4 : a.M), block(NT == 64 ? 256 : NT);
-  if (a.y_type == kF32) hipLaunchKernelGGL((block_norm_kernel<XF32, kF32, NT, CH>), grid, block, 0, st, a);
-  else if (a.y_type == kBF16) hipLaunchKernelGGL((block_norm_kernel<XF32, kBF16, NT, CH>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((block_norm_kernel<XF32, kNone, NT, CH>), grid, block, 0, st, a);
+  constexpr uint32_t kThreads = NT == 64 ? 256 : NT, kRows = NT == 64 ? 4 : 1;
+  const dim3 grid(std::min((a.M + kRows - 1) / kRows, kWaves / (kThreads / 64))), block(kThreads);
+  if (a.layer) hipLaunchKernelGGL((block_norm_kernel<XF32, YT, true, NT, CH>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((block_norm_kernel<XF32, YT, false, NT, CH>), grid, block, 0, st, a);
 }
 template <int NT, int CH>
 void launch(const NormArgs& a, hipStream_t st) {
-  if (a.x_type == kF32) launch<true, NT, CH>(a, st);
-  else launch<false, NT, CH>(a, st);
+  if (a.x_type == kF32) {
+    if (a.y_type == kF32) launch<true, kF32, NT, CH>(a, st);
+    else if (a.y_type == kBF16) launch<true, kBF16, NT, CH>(a, st);
+    else launch<true, kNone, NT, CH>(a, st);
+  } else {
+    if (a.y_type == kF32) launch<false, kF32, NT, CH>(a, st);
+    else if (a.y_type == kBF16) launch<false, kBF16, NT, CH>(a, st);
+    else launch<false, kNone, NT, CH>(a, st);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t st) {
   const uint32_t P = a.K / 8;
+  const bool many = a.M >= 512;
   if (P <= 64) launch<64, 1>(a, st);
-  else if (P <= 128) launch<64, 2>(a, st);
-  else if (P <= 256) launch<256, 1>(a, st);
-  else if (P <= 512) launch<256, 2>(a, st);
-  else if (P <= 1024) launch<1024, 1>(a, st);
-  else if (P <= 2048) launch<1024, 2>(a, st);
-  else if (a.K <= kMostHeld) launch<1024, 4>(a, st);
+  else if (P <= 128) many ? launch<64, 2>(a, st) : launch<128, 1>(a, st);
+  else if (P <= 256) many ? launch<128, 2>(a, st) : launch<256, 1>(a, st);
+  else if (P <= 512) many ? launch<256, 2>(a, st) : launch<512, 1>(a, st);
+  else if (P <= 1024) launch<512, 2>(a, st);
+  else if (a.K <= kMostHeld) launch<512, 4>(a, st);
   else hipLaunchKernelGGL(block_norm_wide, dim3(a.M), dim3(1024), 0, st, a);
   return hipGetLastError();
 }

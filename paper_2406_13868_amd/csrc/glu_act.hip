@@ -97,11 +97,18 @@ __device__ __forceinline__ void values(const GluArgs& a, int64_t row, int64_t k,
   activate<ACT, GATED>(g, u, h);
 }
 
+// NT threads a row, in pieces of eight elements, CH each; a wave's rows are four to a
+// workgroup.  (Workgroups that take row after row, the next on its way, are slower:
+// the fp64 units are the bound, and the registers it takes leave fewer waves for them;
+// 4096 x 11008: 78 us.)
 template <int ACT, bool XF32, bool GATED, int NT, int CH>
-__global__ __launch_bounds__(NT) void glu_code_kernel(GluArgs a) {
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void glu_code_kernel(GluArgs a) {
   __shared__ uint32_t top[NT / 64];
-  const uint32_t t = threadIdx.x, P = a.F / 8;
-  const int64_t m = blockIdx.x, from = m * a.x_stride;
+  const uint32_t t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, P = a.F / 8;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = NT == 64 ? 0 : wave * 64;  // its first piece
+  const uint32_t m = NT == 64 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (m >= a.M) return;  // whole waves, and none that others wait for
+  const int64_t from = int64_t(m) * a.x_stride;
   const bool e4m3 = a.out_type == kE4M3;
   const RowBuf<XF32> gr(a.x, from, a.F), ur(a.x, GATED ? from + a.F : from, a.F);
   Raw8<XF32> gq[CH], uq[CH];
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(NT) void glu_code_kernel(GluArgs a) {
   float h[CH][8], most = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if (c > 0 && __builtin_amdgcn_readfirstlane(t) + c * NT >= P) {  // the whole wave is past the row
+    if (c > 0 && first + c * NT >= P) {  // the whole wave is past the row
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[c][i] = 0.f;
       continue;
@@ -130,7 +137,7 @@ __global__ __launch_bounds__(NT) void glu_code_kernel(GluArgs a) {
 #pragma unroll
   for (int c = 0; c < CH; ++c)
     if (t + c * NT < P)
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + m * a.F + (t + c * NT) * 8) = codes8(h[c], code, e4m3);
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + int64_t(m) * a.F + (t + c * NT) * 8) = codes8(h[c], code, e4m3);
 }
 
 // Rows of any width: the activation is evaluated for the maximum and again for
@@ -170,22 +177,33 @@ __global__ __launch_bounds__(256) void glu_act_kernel(GluArgs a) {
   store8(a.out_type == kF32, a.out, int64_t(m) * a.F + int64_t(p) * 8, h);
 }
 
+template <int ACT, bool XF32, bool GATED, int NT, int CH>
+void rows(const GluArgs& a, hipStream_t st) {
+  const dim3 grid(NT == 64 ? (a.M + 3) / 4 : a.M), block(NT == 64 ? 256 : NT);
+  hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, NT, CH>), grid, block, 0, st, a);
+}
+
 template <int ACT, bool XF32, bool GATED>
 void launch(const GluArgs& a, hipStream_t st) {
   const uint32_t P = a.F / 8;
+  const bool many = a.M >= 512;
   if (a.out_type == kF32 || a.out_type == kBF16) {
     const uint64_t pieces = uint64_t(a.M) * P;
     hipLaunchKernelGGL((glu_act_kernel<ACT, XF32, GATED>), dim3(uint32_t((pieces + 255) / 256)), dim3(256), 0, st, a);
+  } else if (P <= 64) {
+    rows<ACT, XF32, GATED, 64, 1>(a, st);
+  } else if (P <= 128) {
+    many ? rows<ACT, XF32, GATED, 64, 2>(a, st) : rows<ACT, XF32, GATED, 128, 1>(a, st);
   } else if (P <= 256) {
-    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 256, 1>), dim3(a.M), dim3(256), 0, st, a);
+    many ? rows<ACT, XF32, GATED, 64, 4>(a, st) : rows<ACT, XF32, GATED, 256, 1>(a, st);
   } else if (P <= 512) {
-    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 256, 2>), dim3(a.M), dim3(256), 0, st, a);
+    many ? rows<ACT, XF32, GATED, 256, 2>(a, st) : rows<ACT, XF32, GATED, 512, 1>(a, st);
   } else if (P <= 1024) {
-    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 1>), dim3(a.M), dim3(1024), 0, st, a);
+    many ? rows<ACT, XF32, GATED, 256, 4>(a, st) : rows<ACT, XF32, GATED, 1024, 1>(a, st);
   } else if (P <= 2048) {
-    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 2>), dim3(a.M), dim3(1024), 0, st, a);
+    many ? rows<ACT, XF32, GATED, 256, 8>(a, st) : rows<ACT, XF32, GATED, 1024, 2>(a, st);
   } else if (a.F <= kMostHeld) {
-    hipLaunchKernelGGL((glu_code_kernel<ACT, XF32, GATED, 1024, 4>), dim3(a.M), dim3(1024), 0, st, a);
+    rows<ACT, XF32, GATED, 1024, 4>(a, st);
   } else {
     hipLaunchKernelGGL((glu_code_wide<ACT, XF32, GATED>), dim3(a.M), dim3(1024), 0, st, a);
   }
