@@ -21,28 +21,31 @@ _GLU = struct.Struct("@3P3q4i0q")
 _INT8 = struct.Struct("@7PN6qi0q")
 
 # A call's host time is its floor at decode sizes, and most of it is spent on
-# asking tensors what they are: each is asked once, and what does not fit is named
-# by the functions below, off the straight path.
-_OUT = {}      # out_dtype, as a name or a torch dtype, and the dtype of the tensor and the library's type for it
-_KIND = {}     # torch dtype of activations: the library's type
-_stream_of = _device_now = None
+# asking tensors what they are: each is asked once and in place, and what does not
+# fit is named by the functions below, off the straight path.
+_OUT = {}   # out_dtype, as a name or a torch dtype: the dtype of the tensor and the library's type for it
+_KIND = {}  # torch dtype of activations: the library's type
+_f32 = _i8 = _u8 = _stream_of = _device_now = _norm = _glu = _int8 = None
+_CODES = _lib.DTYPE_E4M3  # the library's types from here on are codes
 
 
 def _prepare():
-    """What the calls need of torch, looked up once."""
-    global _stream_of, _device_now
-    torch = _torch()
+    """What the calls need of torch and the library, looked up once."""
+    global _f32, _i8, _u8, _stream_of, _device_now, _norm, _glu, _int8
+    torch, lib = _torch(), _lib.lib()
+    _norm, _glu, _int8 = lib.sdq_block_norm, lib.sdq_glu_act, lib.sdq_gemm_int8
+    _i8, _u8 = torch.int8, torch.uint8
     _KIND.update({torch.float32: _lib.DTYPE_F32, torch.bfloat16: _lib.DTYPE_BF16})
-    _OUT.update({"int8": (torch.uint8, _lib.DTYPE_INT8), "e4m3": (torch.uint8, _lib.DTYPE_E4M3)})
+    _OUT.update({"int8": (_u8, _lib.DTYPE_INT8), "e4m3": (_u8, _lib.DTYPE_E4M3)})
     for name, dt in (("f32", torch.float32), ("bf16", torch.bfloat16)):
         _OUT[name] = _OUT[dt] = (dt, _KIND[dt])
     _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _f32 = torch.float32  # last: it says that all of them are there
 
 
-def _run(name, packed, index, stream):
+def _run(fn, packed, index, stream, name):
     """The library's call on the given stream, or the current one of the tensors' device, with that device current."""
-    fn = getattr(_lib._lib or _lib.lib(), name)
     if _device_now() != index:
         with _torch().cuda.device(index):
             rc = fn(packed, _stream_of(index) if stream is None else stream.cuda_stream)
@@ -52,20 +55,18 @@ def _run(name, packed, index, stream):
         _lib.check(rc, name)
 
 
-def _wrong(t, what, M=None, K=None, dtype=None, index=None):
+def _wrong(t, what, M=None, K=None, index=None, kinds="float32 or bfloat16"):
     """Raises what is wrong with a tensor that should have rows [M, K] on a GPU."""
     torch = _torch()
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{what} must be a two-dimensional tensor")
     if M is not None and t.shape != (M, K):
         raise ValueError(f"{what} must be [{M}, {K}], got {list(t.shape)}")
-    if dtype is not None and t.dtype is not dtype:
-        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
     if not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{what} must be a CUDA (HIP) tensor with contiguous rows")
     if index is not None and t.get_device() != index:
         raise ValueError(f"{what} is on another device: {t.device}")
-    raise ValueError(f"{what} must be float32 or bfloat16")
+    raise ValueError(f"{what} must be {kinds}, got {t.dtype}")
 
 
 def _first(t, what):
@@ -79,7 +80,7 @@ def _first(t, what):
         _wrong(t, what)
     if index < 0 or (step != 1 and K > 1):
         _wrong(t, what)
-    if _stream_of is None:
+    if _f32 is None:
         _prepare()
     return shape, M, K, ld if M > 1 else K, t.data_ptr(), index
 
@@ -98,13 +99,12 @@ def _like(t, shape, what, index):
 
 def _vec(t, n, what, index):
     """The address of an fp32 vector of n elements."""
-    torch = _torch()
     try:
-        if t.dtype is torch.float32 and t.shape == (n,) and t.get_device() == index and t.is_contiguous():
+        if t.dtype is _f32 and t.shape == n and t.get_device() == index and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
         pass
-    _dev(_need(t, (n,), torch.float32, what), what)
+    _dev(_need(t, n, _f32, what), what)
     raise ValueError(f"{what} is on another device: {t.device}")
 
 
@@ -115,22 +115,21 @@ def _kind(t, what):
         raise ValueError(f"{what} must be float32 or bfloat16") from None
 
 
-def _result(out, scales, out_dtype, shape, default, like, index, stream):
+def _result(out, scales, out_dtype, shape, rows, like, index, stream):
     """The output of a call: the tensor, the library's type for it, and for codes the scales and their address."""
     if out_dtype is None:
-        out_dtype = default if out is None else out.dtype
+        out_dtype = like.dtype if out is None else out.dtype
     try:
         want, code = _OUT[out_dtype]
     except (KeyError, TypeError):
         raise ValueError("out_dtype must be 'int8', 'e4m3', 'bf16', 'f32' or a torch dtype of the last two") from None
-    if code >= _lib.DTYPE_E4M3:
+    at = 0
+    if code >= _CODES:
         if scales is None:
-            scales = _empty(shape[:1], _torch().float32, like.device, stream)
-        at = _vec(scales, shape[0], "scales", index)
+            scales = _empty(rows, _f32, like.device, stream)
+        at = _vec(scales, rows, "scales", index)
     elif scales is not None:
         raise ValueError("scales belong to codes")
-    else:
-        at = 0
     if out is None:
         out = _empty(shape, want, like.device, stream)
     elif out.dtype is not want or out.shape != shape or out.get_device() != index or not out.is_contiguous():
@@ -158,7 +157,7 @@ def block_norm(residual, y=None, weight=None, bias=None, eps: float = 1e-6, laye
     for uint8 codes and their scales, the Xq and s_a of the products; scales is
     None otherwise.  post_eps defaults to eps."""
     shape, M, K, ld, at, index = _first(residual, "residual")
-    kind = _kind(residual, "residual")
+    cols, kind = (K,), _kind(residual, "residual")
     y_at = y_ld = y_kind = to = to_ld = 0
     gate_at = gate_ld = gate_kind = per_row = 0
     if y is not None:
@@ -168,24 +167,33 @@ def block_norm(residual, y=None, weight=None, bias=None, eps: float = 1e-6, laye
             residual_out = _empty(shape, residual.dtype, residual.device, stream)
         to_ld, to = _like(residual_out, shape, "residual_out", index)
         if residual_out.dtype is not residual.dtype:
-            _wrong(residual_out, "residual_out", M, K, residual.dtype)
+            _wrong(residual_out, "residual_out", kinds=residual.dtype)
         if gate is not None:
             gate_at, gate_ld, gate_kind, per_row = _gate(gate, M, K, index)
     elif gate is not None or post_weight is not None or post_bias is not None or residual_out is not None:
         raise ValueError("gate, post_weight, post_bias and residual_out belong to y")
     if weight is not None:
-        out, code, scales, scales_at = _result(out, scales, out_dtype, shape, residual.dtype, residual, index, stream)
-        out_at, weight_at = out.data_ptr(), _vec(weight, K, "weight", index)
+        out, code, scales, scales_at = _result(out, scales, out_dtype, shape, (M,), residual, index, stream)
+        out_at, weight_at = out.data_ptr(), _vec(weight, cols, "weight", index)
     elif y is None or out is not None or bias is not None or scales is not None or out_dtype is not None:
         raise ValueError("out, out_dtype, scales and bias belong to weight, and without y there must be one")
     else:
         code = scales_at = out_at = weight_at = 0
+    bias_at = post_at = post_bias_at = 0
+    if bias is not None:
+        bias_at = _vec(bias, cols, "bias", index)
+    if post_weight is not None:
+        post_at = _vec(post_weight, cols, "post_weight", index)
+        if post_bias is not None:
+            post_bias_at = _vec(post_bias, cols, "post_bias", index)
+        if post_eps is None:
+            post_eps = eps
+    elif post_bias is not None:
+        raise ValueError("post_bias belongs to post_weight")
     if M:
-        _run("sdq_block_norm", _NORM.pack(
-            at, y_at, gate_at, weight_at, 0 if bias is None else _vec(bias, K, "bias", index),
-            0 if post_weight is None else _vec(post_weight, K, "post_weight", index),
-            0 if post_bias is None else _vec(post_bias, K, "post_bias", index), to, out_at, scales_at, M, K, ld, y_ld, gate_ld,
-            to_ld, eps, eps if post_eps is None else post_eps, kind, y_kind, gate_kind, code, per_row, layer, scale), index, stream)
+        _run(_norm, _NORM.pack(at, y_at, gate_at, weight_at, bias_at, post_at, post_bias_at, to, out_at, scales_at, M, K, ld, y_ld,
+                               gate_ld, to_ld, eps, post_eps or 0.0, kind, y_kind, gate_kind, code, per_row, layer, scale),
+             index, stream, "sdq_block_norm")
     return residual if y is None else residual_out, out, scales
 
 
@@ -227,9 +235,9 @@ def glu_act(x, act: str = "silu", gated: bool = True, out_dtype=None, out=None, 
     if code is None:
         raise ValueError("act must be 'silu', 'gelu' or 'relu'")
     kind = _kind(x, "x")
-    out, to, scales, scales_at = _result(out, scales, out_dtype, shape, x.dtype, x, index, stream)
+    out, to, scales, scales_at = _result(out, scales, out_dtype, shape, (M,), x, index, stream)
     if M:
-        _run("sdq_glu_act", _GLU.pack(at, out.data_ptr(), scales_at, M, F, ld, kind, to, code, gated), index, stream)
+        _run(_glu, _GLU.pack(at, out.data_ptr(), scales_at, M, F, ld, kind, to, code, gated), index, stream, "sdq_glu_act")
     return out, scales
 
 
@@ -250,16 +258,18 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
     int8 activations, once.  out: [M, N], fp32 or bf16, rows may be strided; or
     out_dtype (default fp32).  workspace: a uint8 tensor of gemm_int8_workspace_size
     bytes, or a fresh one is made where that is not 0."""
-    torch = _torch()
     _, M, K, x_ld, x_at, index = _first(xq, "xq")
     _, N, depth, w_ld, w_at, where = _first(wq, "wq")
-    for t, what in ((xq, "xq"), (wq, "wq")):
-        if t.dtype is not torch.int8 and t.dtype is not torch.uint8:
-            raise ValueError(f"{what} must be int8 codes (int8 or uint8)")
     if depth != K or where != index:
         _wrong(wq, "wq", N, K, index=index)
+    dt = xq.dtype
+    if dt is not _i8 and dt is not _u8:
+        _wrong(xq, "xq", kinds="int8 codes (int8 or uint8)")
+    dt = wq.dtype
+    if dt is not _i8 and dt is not _u8:
+        _wrong(wq, "wq", kinds="int8 codes (int8 or uint8)")
     if out is None:
-        out = _empty((M, N), torch.float32 if out_dtype is None else out_dtype, xq.device, stream)
+        out = _empty((M, N), _f32 if out_dtype is None else out_dtype, xq.device, stream)
     elif out_dtype is not None and out.dtype is not out_dtype:
         raise ValueError(f"out must be {out_dtype}")
     y_ld, y_at = _like(out, (M, N), "out", index)
@@ -271,9 +281,9 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
         elif _need_bytes(workspace, need, "workspace").get_device() != index:
             raise ValueError(f"workspace is on another device: {workspace.device}")
         ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    packed = _INT8.pack(
-        x_at, w_at, _vec(s_x, M, "s_x", index), _vec(s_w, N, "s_w", index), 0 if bias is None else _vec(bias, N, "bias", index), y_at,
-        ws, ws_bytes, M, N, K, x_ld, w_ld, y_ld, _kind(out, "out"))
+    bias_at = 0 if bias is None else _vec(bias, (N,), "bias", index)
+    packed = _INT8.pack(x_at, w_at, _vec(s_x, (M,), "s_x", index), _vec(s_w, (N,), "s_w", index), bias_at, y_at, ws, ws_bytes, M, N, K,
+                        x_ld, w_ld, y_ld, _kind(out, "out"))
     if M:
-        _run("sdq_gemm_int8", packed, index, stream)
+        _run(_int8, packed, index, stream, "sdq_gemm_int8")
     return out

@@ -112,7 +112,7 @@ def test_products_divided_over_their_depth(M, N, K):
         call = _lib.sdq_int8_args(xq=args[0].data_ptr(), wq=args[2].data_ptr(), s_x=args[1].data_ptr(), s_w=args[3].data_ptr(),
                                   bias=bias.data_ptr(), y=z.data_ptr(), M=M, N=N, K=K, x_stride=K, w_stride=K, y_stride=N,
                                   y_dtype=int(dt is torch.bfloat16))
-        block._run("sdq_gemm_int8", bytes(call), 0, None)
+        block._run(_lib.lib().sdq_gemm_int8, bytes(call), 0, None, "sdq_gemm_int8")
         assert torch.equal(z, y)
     with pytest.raises(ValueError, match="workspace holds"):
         sdq.gemm_int8(*args, workspace=ws[: need - 16])
