@@ -241,17 +241,15 @@ __global__ __launch_bounds__(256) void gemm_int8_join(Int8Args a, const int32_t*
 }
 
 // ---- few tokens ------------------------------------------------------------
-// Up to 64 tokens, whose time is that of the weights' bytes.  A workgroup takes one
-// tile of 16 outputs and all tokens after the other; its waves take a tile's
-// 128-byte units of K in turn, and their sums meet in shared memory.  A wave waits
-// for the others at the end of a tile only, with the next tile's units on their way.
-//
-// Whole pieces of rows are requested, into registers, DEPTH units ahead: there is
-// more room than in shared memory, and loads return in order, so that tokens, which
-// the L2 holds, would wait for weights requested before them.  From there they pass
-// through shared memory of the wave's own into the operands' order.  (Requested in
-// that order, lanes that follow each other take four rows, which costs the address
-// units three times as much: 2.9 TB/s with 16 tokens, 1.4 with 64.)
+// Up to 32 tokens, whose time is that of the weights' bytes.  A workgroup takes one
+// tile of outputs and all tokens after the other; its waves take a tile's 128-byte
+// units of K in turn.  Each wave has a ring of three units in shared memory, of which
+// two are on their way while one is multiplied, the next tile's among them: it waits
+// for the others only where a tile ends, and their sums are added up in shared memory
+// by integer atomics.  Whole lines of rows are requested, in the order that spreads
+// them over the banks.  (In the operands' own order, straight to registers, lanes
+// that follow each other take four rows, which costs the address units three times as
+// much: 2.9 TB/s with 16 tokens.)
 //
 // 16x16x64: A = 16 rows of W, B = 16 tokens, 16 bytes of K a lane (lane l: row or
 // token l & 15, bytes 16 (l >> 4)); the sums leave a lane four outputs of a token.
@@ -321,7 +319,7 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_int8_few(Int8Args a) {
 #pragma unroll
   for (int s = 0; s < 2; ++s) from[s] = i16 * kChunk + (((4 * s + g) ^ (i16 >> 1 & 7)) << 4);
 
-  // the sums of the waves, by the first MT of them: a tile of 16 tokens each
+  // a wave finishes every WAVES-th tile of 16 outputs by 16 tokens
   int tile = blockIdx.x, unit = wave, count = 0;
   constexpr int kSums = (MT * NT + WAVES - 1) / WAVES;
   float sx[kSums];
@@ -469,8 +467,10 @@ constexpr Form kForms[] = {{64, 64, .22, .46, .30, .63},
 struct Choice { int form, parts; };
 
 // K divided over `parts` workgroups costs a second launch and the sums' way through
-// memory: 3 microseconds, and 4 TB/s of them written and read.  (64 x 4096 x 16384:
-// 26.6 us undivided, 17.0 in 4 parts.)
+// memory: 3 microseconds, and 4 TB/s of them written and read; and it never takes
+// less than the host needs for a call of two launches, 9.  (64 x 4096 x 16384:
+// 26.6 us undivided, 17.0 in 4 parts; 37 x 51 x 3712, called from Python: 11.2 in
+// 4 parts with a workspace of the call's own, 8.5 undivided.)
 Choice choose(int64_t M, int64_t N, int64_t K, bool divide) {
   const int chunks = int((K + kChunk - 1) / kChunk);
   Choice best{0, 1};
@@ -485,7 +485,7 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool divide) {
       const int64_t all = tiles * parts, rest = all % round;
       const double whole = part * two + 2, some = part * one + 2;
       double t = double(all / round) * whole + (rest == 0 ? 0 : rest <= 256 ? some : whole);
-      if (parts > 1) t = 1.1 * (t + 3 + double(M) * double(N) * (8 * parts + 4) / 4e6);
+      if (parts > 1) t = std::max(1.1 * (t + 3 + double(M) * double(N) * (8 * parts + 4) / 4e6), 9.0);
       if (t < least) {
         least = t;
         best = {f, parts};
@@ -495,7 +495,9 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool divide) {
   return best;
 }
 
-bool few_tokens(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 8192); }
+// Measured: 20 x 512 x 4096: 4.9 us, 8.6 by tiles; 32 x 4096 x 4096: 7.7 and 10;
+// 32 x 8192 x 4096: 13.4 and 10.5.
+bool few_tokens(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 4096); }
 
 }  // namespace
 
