@@ -117,6 +117,8 @@ def _kind(t, what):
 
 def _result(out, scales, out_dtype, shape, rows, like, index, stream):
     """The output of a call: the tensor, the library's type for it, and for codes the scales and their address."""
+    if out is not None and not hasattr(out, "get_device"):
+        raise ValueError("out must be a torch tensor")
     if out_dtype is None:
         out_dtype = like.dtype if out is None else out.dtype
     try:
@@ -207,8 +209,8 @@ def _gate(gate, M, K, index):
     if gate.get_device() != index:
         raise ValueError(f"gate is on another device: {gate.device}")
     ld = per_row = 0
-    if shape == (M, K) and M > 1:
-        ld = stride[0]
+    if shape == (M, K):
+        ld = stride[0] if M > 1 else 0
     elif shape == (M, 1):
         ld, per_row = stride[0] if M > 1 else 0, 1
     elif shape != (K,) and shape != (1, K):

@@ -114,3 +114,27 @@ def test_the_binding_checks_the_calls():
     q = torch.zeros((3, 64), dtype=torch.int8)
     _raises(lambda: sdq.gemm_int8(q[0], r[:, 0], q, r[:, 0]), "xq must be")
     _raises(lambda: sdq.gemm_int8(q, r[:, 0], q, r[:, 0]), "CUDA")
+
+
+def test_the_shapes_that_a_gate_may_have():
+    """The address, row stride, type and kind of each form; tensors here lie on no GPU, whose index is -1."""
+    block._prepare()
+    K = 16
+    for M in (0, 1, 3):
+        for t, ld, per_row in ((torch.zeros(K), 0, 0), (torch.zeros(1, K), 0, 0), (torch.zeros(M, K), K if M > 1 else 0, 0),
+                               (torch.zeros(M, 1), 1 if M > 1 else 0, 1), (torch.zeros(M, K + 8)[:, :K], K + 8 if M > 1 else 0, 0),
+                               (torch.zeros(1, K).expand(M, K), 0, 0)):
+            assert block._gate(t, M, K, -1) == (t.data_ptr(), ld, _lib.DTYPE_F32, per_row)
+    for t in (torch.zeros(3, K + 8), torch.zeros(2, K), torch.zeros(2, 1), torch.zeros(8)):
+        _raises(lambda: block._gate(t, 3, K, -1), "gate must be")
+    _raises(lambda: block._gate(torch.zeros(3, 2 * K)[:, ::2], 3, K, -1), "contiguous")
+    _raises(lambda: block._gate([1.0], 3, K, -1), "torch tensor")
+    _raises(lambda: block._gate(torch.zeros(K), 3, K, 0), "another device")
+
+
+def test_outputs_that_are_no_tensors():
+    block._prepare()
+    like = torch.zeros(3, 16)
+    for out_dtype in (None, "int8", "bf16"):
+        scales = torch.zeros(3) if out_dtype == "int8" else None
+        _raises(lambda: block._result([1.0], scales, out_dtype, (3, 16), (3,), like, -1, None), "out must be a torch tensor")
