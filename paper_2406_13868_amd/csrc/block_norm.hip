@@ -349,12 +349,19 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
 // Workgroups of 256 compute units' worth of waves, each taking rows in turn.
 constexpr uint32_t kWaves = 256 * 16;
 
-template <bool XF32, int YT, int NT, int CH>
-void launch(const NormArgs& a, hipStream_t st) {
+template <bool XF32, int YT, bool LAYER, int NT, int CH>
+void launch_rows(const NormArgs& a, hipStream_t st) {
   constexpr uint32_t kThreads = NT == 64 ? 256 : NT, kRows = NT == 64 ? 4 : 1;
   const dim3 grid(std::min((a.M + kRows - 1) / kRows, kWaves / (kThreads / 64))), block(kThreads);
-  if (a.layer) hipLaunchKernelGGL((block_norm_kernel<XF32, YT, true, NT, CH>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((block_norm_kernel<XF32, YT, false, NT, CH>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((block_norm_kernel<XF32, YT, LAYER, NT, CH>), grid, block, 0, st, a);
+}
+template <bool XF32, int YT, int NT, int CH>
+void launch(const NormArgs& a, hipStream_t st) {
+  // 1024 threads have 128 registers each: a layer norm's weights and biases, or an fp32
+  // block's rows, would leave them (1024 x 16384, fp32: 68 us; 60 with 512 threads).
+  constexpr bool kMost = NT == 1024;
+  if (a.layer) launch_rows<XF32, YT, true, kMost ? 512 : NT, kMost ? 2 * CH : CH>(a, st);
+  else launch_rows<XF32, YT, false, kMost && YT == kF32 ? 512 : NT, kMost && YT == kF32 ? 2 * CH : CH>(a, st);
 }
 template <int NT, int CH>
 void launch(const NormArgs& a, hipStream_t st) {
@@ -372,6 +379,13 @@ void launch(const NormArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t st) {
+  // The fewest registers a thread that hold a row, so that few rows end soonest; of many
+  // rows two pieces a thread, where half as many threads meet for a row's sums.  Measured
+  // (bf16, post-norm, gates, int8 codes; the form taken, then the other):
+  //   64 x 1024: 3.1 us (128 threads of one piece), 3.3;  8192 x 1024: 14.9, 16.4
+  //   64 x 4096: 3.7 (512 of one), 3.9;  512 x 4096: 6.1, 6.1;  8192 x 4096: 52.7, 55.5
+  //   64 x 8192: 4.7 (512 of two), 5.0 (1024 of one);  4096 x 8192: 53.2, 61.2
+  //   64 x 16384: 6.6 (1024 of two), 6.5 (512 of four);  2048 x 16384: 57.4, 67.3
   const uint32_t P = a.K / 8;
   const bool many = a.M >= 512;
   if (P <= 64) launch<64, 1>(a, st);
@@ -379,7 +393,7 @@ hipError_t launch_block_norm(const NormArgs& a, hipStream_t st) {
   else if (P <= 256) many ? launch<128, 2>(a, st) : launch<256, 1>(a, st);
   else if (P <= 512) many ? launch<256, 2>(a, st) : launch<512, 1>(a, st);
   else if (P <= 1024) launch<512, 2>(a, st);
-  else if (a.K <= kMostHeld) launch<512, 4>(a, st);
+  else if (a.K <= kMostHeld) launch<1024, 2>(a, st);
   else hipLaunchKernelGGL(block_norm_wide, dim3(a.M), dim3(1024), 0, st, a);
   return hipGetLastError();
 }

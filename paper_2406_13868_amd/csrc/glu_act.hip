@@ -185,6 +185,14 @@ void rows(const GluArgs& a, hipStream_t st) {
 
 template <int ACT, bool XF32, bool GATED>
 void launch(const GluArgs& a, hipStream_t st) {
+  // Few rows end soonest on many threads, as long as no wave waits for many others; many
+  // rows keep the fp64 units busiest with few threads, of which some workgroups load
+  // while others compute.  Measured (bf16, gated silu, int8 codes; the form taken, then
+  // the other):
+  //   64 x 2048: 3.1 us (256 threads of one piece), 4.8;  8192 x 2048: 24.6 (64 of four), 35.1
+  //   1 x 4096: 3.1 (256 of two), 3.4 (512 of one);  8192 x 4096: 46.4, 74.9
+  //   1 x 8192: 4.0 (512 of two), 4.6 (256 of four);  4096 x 8192: 48.1 (256 of four), 74.8 (1024 of one)
+  //   1 x 11008: 4.7 (1024 of two), 6.3;  4096 x 11008: 63.0 (256 of eight), 81.6
   const uint32_t P = a.F / 8;
   const bool many = a.M >= 512;
   if (a.out_type == kF32 || a.out_type == kBF16) {
@@ -197,9 +205,9 @@ void launch(const GluArgs& a, hipStream_t st) {
   } else if (P <= 256) {
     many ? rows<ACT, XF32, GATED, 64, 4>(a, st) : rows<ACT, XF32, GATED, 256, 1>(a, st);
   } else if (P <= 512) {
-    many ? rows<ACT, XF32, GATED, 256, 2>(a, st) : rows<ACT, XF32, GATED, 512, 1>(a, st);
+    rows<ACT, XF32, GATED, 256, 2>(a, st);
   } else if (P <= 1024) {
-    many ? rows<ACT, XF32, GATED, 256, 4>(a, st) : rows<ACT, XF32, GATED, 1024, 1>(a, st);
+    many ? rows<ACT, XF32, GATED, 256, 4>(a, st) : rows<ACT, XF32, GATED, 512, 2>(a, st);
   } else if (P <= 2048) {
     many ? rows<ACT, XF32, GATED, 256, 8>(a, st) : rows<ACT, XF32, GATED, 1024, 2>(a, st);
   } else if (a.F <= kMostHeld) {
