@@ -68,6 +68,14 @@ constexpr int kSums = 4;  // beside kF32 and kBF16: int32 sums, not scaled yet
 // (their results are not stored), and the pieces of 16 past the end of K are the last
 // piece again, with zeros in their place on the tokens' side.
 //
+// What bounds a large product is the way of the tiles' bytes to the compute units, which
+// takes 18 bytes a clock each from the L2s with a quarter of the lines missing there: the
+// requests alone are 327 us of 4096 x 22016 x 4096 in tiles of 256 x 256, the matrix
+// instructions alone 220 to 250 (the clock falls under them).  256 x 384 is the largest
+// tile whose sums, operands and two chunks fit: it asks for a sixth less, and the whole
+// is 335 us, 2.2 POP/s (256 x 256: 369; the library's product of the codes: 339 to 355).
+// Deeper stages of half chunks, and four waves of 128 x 128: no faster.
+//
 // In a stage, row r's piece p (16 bytes) lies at r * 128 + 16 * (p ^ (r / 2 & 7)):
 // the 16 lanes that read a piece of 16 rows together touch every bank once.
 template <int BM, int BN, int STAGES>
@@ -92,10 +100,11 @@ __device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, 
     const int j = i < kA ? i : i - kA, r = (j * kWaves + wave) * 8 + (lane >> 3);
     at[i] = (i < kA ? uint32_t(min(r, rows - 1)) * uint32_t(a.x_stride) : uint32_t(min(r, outs - 1)) * uint32_t(a.w_stride)) + piece(j);
   }
-  // no branch around the requests: as many are on their way at every wait
-  const auto request = [&](int c, uint8_t* s) {
+  // the requests [lo, hi) of chunk c, without a branch around them: as many are on their way at every wait
+  const auto request = [&](int c, uint8_t* s, int lo, int hi) {
 #pragma unroll
     for (int i = 0; i < kA + kB; ++i) {
+      if (i < lo || i >= hi) continue;
       const int j = i < kA ? i : i - kA;
       const uint32_t v = c > last ? kNowhere : at[i] + (c == last ? min(piece(j), left - 16) - piece(j) : 0);
       request_1k(i < kA ? xr : wr, s + (i < kA ? 0 : BM * kChunk) + (j * kWaves + wave) * 1024, v, uint32_t(min(c, last)) * kChunk);
@@ -114,20 +123,6 @@ __device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, 
 #pragma unroll
   for (int s = 0; s < 4; ++s) from[s] = col * kChunk + (((2 * s + h) ^ (col >> 1 & 7)) << 4);
 
-  struct Step { i4 a[MS], b[NS]; };
-  Step f[2];
-  const auto read = [&](const uint8_t* s, int t, Step& to) {
-#pragma unroll
-    for (int j = 0; j < NS; ++j) to.b[j] = *reinterpret_cast<const i4*>(s + (BM + wn + j * 32) * kChunk + from[t]);
-#pragma unroll
-    for (int i = 0; i < MS; ++i) to.a[i] = *reinterpret_cast<const i4*>(s + (wm + i * 32) * kChunk + from[t]);
-  };
-  const auto multiply = [&](const Step& x) {
-#pragma unroll
-    for (int i = 0; i < MS; ++i)
-#pragma unroll
-      for (int j = 0; j < NS; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.a[i], x.b[j], acc[i][j], 0, 0, 0);
-  };
   // Chunk c, requested into s, has arrived there for every wave; and every wave has
   // read what it reads of the chunk before.
   const auto arrive = [&](int c, uint8_t* s) {
@@ -139,30 +134,88 @@ __device__ __forceinline__ void tile_product(const Int8Args& a, int m0, int n0, 
     }
     barrier_lds();
   };
-  // Each step's operands are read while the step before is multiplied, and the next
-  // chunk is awaited before the last step, so that a chunk begins on operands in
-  // registers.
+  constexpr int kReq = kA + kB;
+  const auto read_a = [&](const uint8_t* s, int t, int i) { return *reinterpret_cast<const i4*>(s + (wm + i * 32) * kChunk + from[t]); };
+  const auto read_b = [&](const uint8_t* s, int t, int j) { return *reinterpret_cast<const i4*>(s + (BM + wn + j * 32) * kChunk + from[t]); };
+  const auto multiply = [&](const i4& x, const i4& w, i16v& to) { to = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, w, to, 0, 0, 0); };
 #pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i) request(i, mem + i * kStage);
+  for (int i = 0; i < STAGES - 1; ++i) request(i, mem + i * kStage, 0, kReq);
   arrive(0, mem);
-  request(STAGES - 1, mem + (STAGES - 1) * kStage);
-  read(mem, 0, f[0]);
-  for (int c = 0;;) {
+  if constexpr (MS * NS < 8) {
+    // Each step's operands are read while the step before is multiplied, and the next
+    // chunk is awaited before the last step, so that a chunk begins on operands in
+    // registers.
+    i4 xa[2][MS], xb[2][NS];
+    const auto read = [&](const uint8_t* s, int t, int to) {
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i) {  // the stage's place is a constant of the reads
-      uint8_t *const s = mem + i * kStage, *const next = mem + (i + 1) % STAGES * kStage;
+      for (int j = 0; j < NS; ++j) xb[to][j] = read_b(s, t, j);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t == 3) {
-          arrive(c + 1, next);
-          request(c + STAGES, s);
+      for (int i = 0; i < MS; ++i) xa[to][i] = read_a(s, t, i);
+    };
+    request(STAGES - 1, mem + (STAGES - 1) * kStage, 0, kReq);
+    read(mem, 0, 0);
+    for (int c = 0;;) {
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) {  // the stage's place is a constant of the reads
+        uint8_t *const s = mem + i * kStage, *const next = mem + (i + 1) % STAGES * kStage;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if (t == 3) {
+            arrive(c + 1, next);
+            request(c + STAGES, s, 0, kReq);
+          }
+          read(t < 3 ? s : next, (t + 1) & 3, (t + 1) & 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int k = 0; k < MS * NS; ++k) multiply(xa[t & 1][k / NS], xb[t & 1][k % NS], acc[k / NS][k % NS]);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        read(t < 3 ? s : next, (t + 1) & 3, f[(t + 1) & 1]);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(f[t & 1]);
-        __builtin_amdgcn_sched_barrier(0);
+        if (++c == chunks) goto multiplied;
       }
-      if (++c == chunks) goto multiplied;
+    }
+  } else {
+    // Between a step's products, one operand of the next step is read or one piece of a
+    // chunk requested at a time: all at once they would wait for each other with the
+    // matrix cores idle.  The weights' operands have two places in registers; a token
+    // operand's is read into when its last product is on its way, the last one's at the
+    // beginning of its own step.  The next chunk is awaited within the last step.
+    constexpr int kProducts = MS * NS, kHalf = kReq / 2, kJoin = 2;
+    i4 xa[MS], xb[2][NS];
+    request(STAGES - 1, mem + (STAGES - 1) * kStage, 0, kHalf);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) xb[0][j] = read_b(mem, 0, j);
+#pragma unroll
+    for (int i = 0; i < MS - 1; ++i) xa[i] = read_a(mem, 0, i);
+    for (int c = 0;;) {
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) {
+        uint8_t *const s = mem + i * kStage, *const next = mem + (i + 1) % STAGES * kStage, *const before = mem + (i + STAGES - 1) % STAGES * kStage;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          // addresses anew at each step: kept, they would take a register for each step and 64 KB
+          uint32_t at0 = from[0] ^ t * 32, at1 = from[0] ^ ((t + 1) & 3) * 32;
+          asm volatile("" : "+v"(at0), "+v"(at1));
+          xa[MS - 1] = *reinterpret_cast<const i4*>(s + (wm + (MS - 1) * 32) * kChunk + at0);
+          __builtin_amdgcn_sched_barrier(0);
+          // the step's first products come before the next chunk is awaited
+          const int first = t == 3 ? kJoin : 0;
+          const uint8_t* const from_next = t == 3 ? next : s;
+#pragma unroll
+          for (int k = 0; k < kProducts; ++k) {
+            if (t == 3 && k == kJoin) arrive(c + 1, next);
+            multiply(xa[k / NS], xb[t & 1][k % NS], acc[k / NS][k % NS]);
+            const int slot = k - first;
+            if (slot >= 0 && slot < NS) xb[(t + 1) & 1][slot] = *reinterpret_cast<const i4*>(from_next + (BM + wn + slot * 32) * kChunk + at1);
+#pragma unroll
+            for (int r = 0; r < MS - 1; ++r)
+              if (k == (r * NS + NS - 1 > first + NS - 1 + r ? r * NS + NS - 1 : first + NS - 1 + r)) xa[r] = *reinterpret_cast<const i4*>(from_next + (wm + r * 32) * kChunk + at1);
+            if (t == 3 && slot >= 0) request(c + STAGES, s, slot * kHalf / (kProducts - kJoin), (slot + 1) * kHalf / (kProducts - kJoin));
+            if (t == 0) request(c + STAGES - 1, before, kHalf + k * (kReq - kHalf) / kProducts, kHalf + (k + 1) * (kReq - kHalf) / kProducts);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        if (++c == chunks) goto multiplied;
+      }
     }
   }
 multiplied:
@@ -173,31 +226,35 @@ multiplied:
   if (have <= 0) return;
   const __amdgpu_buffer_rsrc_t yr =
       buffer_rsrc(static_cast<uint8_t*>(a.y) + ((m0 + wm) * a.y_stride) * es, uint32_t((have - 1) * a.y_stride + a.N) * es);
-  RowScales<MS> rs;
-  if constexpr (OUT != kSums) rs = load_row_scales<MS>(a.s_x, a.M, m0 + wm, h);
+  float sw[NS], bias[NS];
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
-    const int n = n0 + wn + j * 32 + col;
-    if (n >= a.N) continue;
-    float sw = 0.f, b = 0.f;
-    if constexpr (OUT != kSums) {
-      sw = a.s_w[n];
-      if (a.bias) b = a.bias[n];
-    }
+    const int n = min(n0 + wn + j * 32 + col, a.N - 1);
+    sw[j] = OUT == kSums ? 0.f : a.s_w[n];
+    bias[j] = OUT != kSums && a.bias ? a.bias[n] : 0.f;
+  }
 #pragma unroll
-    for (int i = 0; i < MS; ++i)
+  for (int i = 0; i < MS; ++i) {
+    if (m0 + wm + i * 32 >= a.M) break;
+    RowScales<1> rs;
+    if constexpr (OUT != kSums) rs = load_row_scales<1>(a.s_x, a.M, m0 + wm + i * 32, h);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      const int n = n0 + wn + j * 32 + col;
+      if (n >= a.N) continue;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const uint32_t idx = uint32_t(i * 32 + tile_row(e, h)) * uint32_t(a.y_stride) + uint32_t(n);
         if constexpr (OUT == kSums) {
           __builtin_amdgcn_raw_buffer_store_b32(uint32_t(acc[i][j][e]), yr, idx * 4u, 0, 0);
         } else {
-          float v = float(acc[i][j][e]) * rs.v[i][e] * sw;
-          if (a.bias) v += b;
+          float v = float(acc[i][j][e]) * rs.v[0][e] * sw[j];
+          if (a.bias) v += bias[j];
           if constexpr (OUT == kBF16) __builtin_amdgcn_raw_buffer_store_b16(bf16_bits(v), yr, idx * 2u, 0, 0);
           else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), yr, idx * 4u, 0, 0);
         }
       }
+    }
   }
 }
 
@@ -455,14 +512,15 @@ hipError_t join(const Int8Args& a, int parts, hipStream_t st) {
 
 // The forms of tiles, and their times in microseconds: in every round of 256 compute
 // units, or twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2
-// for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs, K = 4096
-// and, where rows are not whole cache lines and a chunk of each takes two, 4112.
+// for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs (the last
+// form: 2048 to 16384 by 4096 to 22016), K = 4096 and, where rows are not whole cache lines and a chunk of each takes two, 4112.
 struct Form { int bm, bn; double one, two, one_odd, two_odd; };
 constexpr Form kForms[] = {{64, 64, .22, .46, .30, .63},
                            {64, 128, .42, .80, .53, 1.0},
                            {128, 128, .72, 0, .80, 0},
                            {128, 128, .87, 1.18, 1.04, 1.46},
-                           {256, 256, 1.85, 0, 2.1, 0}};
+                           {256, 256, 1.85, 0, 2.1, 0},
+                           {256, 384, 2.5, 0, 2.9, 0}};
 
 struct Choice { int form, parts; };
 
@@ -518,7 +576,8 @@ hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
     case 1: e = tile<64, 128, 32, 32, 3>(a, c.parts, st); break;
     case 2: e = tile<128, 128, 64, 32, 4>(a, c.parts, st); break;
     case 3: e = tile<128, 128, 64, 64, 2>(a, c.parts, st); break;
-    default: e = tile<256, 256, 128, 64, 2>(a, c.parts, st); break;
+    case 4: e = tile<256, 256, 128, 64, 2>(a, c.parts, st); break;
+    default: e = tile<256, 384, 128, 96, 2>(a, c.parts, st); break;
   }
   if (e != hipSuccess || c.parts == 1) return e;
   return a.N % 4 == 0 ? join<4>(a, c.parts, st) : join<1>(a, c.parts, st);

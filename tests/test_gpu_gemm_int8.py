@@ -85,6 +85,23 @@ def test_the_largest_sums_are_exact(M):
         assert (y.cpu().numpy() == np.float32(total)).all() and abs(total) < 2 ** 31
 
 
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 384, 400, 528, 1296])
+@pytest.mark.parametrize("M,N", [(1025, 18003), (700, 30005), (3900, 4090), (255, 33000)])
+def test_the_largest_tiles(M, N, K):
+    """256 tokens by 256 or 384 outputs a workgroup, with rows, outputs and depths that end inside a tile.  The sums
+    are exact in fp64 too, and each later step is one fp32 operation."""
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    dt = [torch.bfloat16, torch.float32][K // 16 % 2]
+    say(M, N, K, dt)
+    (x, sx, w, sw), bias, _, _ = make(torch, K, M, N, K, x_gap=16 * (N % 2), bias=K % 128 != 0)
+    y = sdq.gemm_int8(x, sx, w, sw, bias=bias, out_dtype=dt)
+    want = (x.double() @ w.double().t()).float() * sx[:, None] * sw
+    if bias is not None:
+        want = want + bias
+    assert torch.equal(y, want.to(dt))
+
+
 DIVIDED = [(64, 4096, 16384), (100, 300, 8208), (40, 37, 13456), (130, 1000, 8192), (33, 4, 4096), (600, 601, 6000)]
 
 
