@@ -73,7 +73,7 @@ constexpr int kSums = 4;  // beside kF32 and kBF16: int32 sums, not scaled yet
 // requests alone are 327 us of 4096 x 22016 x 4096 in tiles of 256 x 256, the matrix
 // instructions alone 220 to 250 (the clock falls under them).  256 x 384 is the largest
 // tile whose sums, operands and two chunks fit: it asks for a sixth less, and the whole
-// is 335 us, 2.2 POP/s (256 x 256: 369; the library's product of the codes: 339 to 355).
+// is 332 us, 2.2 POP/s (256 x 256: 369; the library's product of the codes: 339 to 355).
 // Deeper stages of half chunks, and four waves of 128 x 128: no faster.
 //
 // In a stage, row r's piece p (16 bytes) lies at r * 128 + 16 * (p ^ (r / 2 & 7)):
@@ -513,14 +513,20 @@ hipError_t join(const Int8Args& a, int parts, hipStream_t st) {
 
 // The forms of tiles, and their times in microseconds: in every round of 256 compute
 // units, or twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2
-// for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs (the last
-// form: 2048 to 16384 by 4096 to 22016), K = 4096 and, where rows are not whole cache
-// lines and a chunk of each takes two, 4112.
+// for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs (the wide
+// forms: 256 to 16384 by 4096 to 22016), K = 4096 and, where rows are not whole cache
+// lines and a chunk of each takes two, 4112.  The form taken and the nearest other, at
+// K = 4096: 256 x 22016: 35.5 us (256 x 128), 46.3 (two of 128 x 128); 512 x 22016: 56.6
+// (256 x 192), 61.9 (128 x 384, dropped); 4096 x 4096: 67 (256 x 256), 77 (256 x 128);
+// 2048 x 11008: 84 (256 x 384), 106 (256 x 256); 1024 x 4096: 26 (128 x 128), 32
+// (256 x 128).
 struct Form { int bm, bn; double one, two, one_odd, two_odd; };
 constexpr Form kForms[] = {{64, 64, .22, .46, .30, .63},
                            {64, 128, .42, .80, .53, 1.0},
                            {128, 128, .72, 0, .80, 0},
                            {128, 128, .87, 1.18, 1.04, 1.46},
+                           {256, 128, 1.15, 0, 1.3, 0},
+                           {256, 192, 1.62, 0, 1.85, 0},
                            {256, 256, 1.85, 0, 2.1, 0},
                            {256, 384, 2.5, 0, 2.9, 0}};
 
@@ -578,7 +584,9 @@ hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
     case 1: e = tile<64, 128, 32, 32, 3>(a, c.parts, st); break;
     case 2: e = tile<128, 128, 64, 32, 4>(a, c.parts, st); break;
     case 3: e = tile<128, 128, 64, 64, 2>(a, c.parts, st); break;
-    case 4: e = tile<256, 256, 128, 64, 2>(a, c.parts, st); break;
+    case 4: e = tile<256, 128, 128, 64, 3>(a, c.parts, st); break;
+    case 5: e = tile<256, 192, 64, 96, 2>(a, c.parts, st); break;
+    case 6: e = tile<256, 256, 128, 64, 2>(a, c.parts, st); break;
     default: e = tile<256, 384, 128, 96, 2>(a, c.parts, st); break;
   }
   if (e != hipSuccess || c.parts == 1) return e;

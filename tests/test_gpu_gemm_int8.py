@@ -86,9 +86,9 @@ def test_the_largest_sums_are_exact(M):
 
 
 @pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 384, 400, 528, 1296])
-@pytest.mark.parametrize("M,N", [(1025, 18003), (700, 30005), (3900, 4090), (255, 33000)])
+@pytest.mark.parametrize("M,N", [(1025, 18003), (700, 30005), (3900, 4090), (255, 33000), (2040, 4005)])
 def test_the_largest_tiles(M, N, K):
-    """256 tokens by 256 or 384 outputs a workgroup, with rows, outputs and depths that end inside a tile.  The sums
+    """256 tokens by 128 to 384 outputs a workgroup, with rows, outputs and depths that end inside a tile.  The sums
     are exact in fp64 too, and each later step is one fp32 operation."""
     torch = torch_cuda()
     import paper_2406_13868_amd as sdq
