@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void gemm_int8_join(Int8Args a, const int32_t*
 // by integer atomics.  Whole lines of rows are requested, in the order that spreads
 // them over the banks.  (In the operands' own order, straight to registers, lanes
 // that follow each other take four rows, which costs the address units three times as
-// much: 2.9 TB/s with 16 tokens.)  16 x 22016 x 4096: 18.6 us, 4.9 TB/s; 1 x 4096 x
+// much: 2.9 TB/s with 16 tokens.)  16 x 22016 x 4096: 17.8 us, 5.1 TB/s; 1 x 4096 x
 // 4096: 5.8, of which 3 are the bytes.
 //
 // 16x16x64: A = 16 rows of W, B = 16 tokens, 16 bytes of K a lane (lane l: row or
@@ -477,12 +477,35 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_int8_few(Int8Args a) {
   __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no request into shared memory outlives the workgroup
 }
 
+// As many workgroups, up to one a compute unit, as share the tiles evenly.
 template <int XG, int NT, int WAVES>
-hipError_t few(const Int8Args& a, int groups, hipStream_t st) {
-  const dim3 grid(unsigned(std::min((a.N + 16 * NT - 1) / (16 * NT), groups))), block(WAVES * 64);
+hipError_t few(const Int8Args& a, hipStream_t st) {
+  const int tiles = (a.N + 16 * NT - 1) / (16 * NT), turns = (tiles + 255) / 256;
+  const dim3 grid(unsigned((tiles + turns - 1) / turns)), block(WAVES * 64);
   if (a.y_bf16) hipLaunchKernelGGL((gemm_int8_few<XG, NT, WAVES, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((gemm_int8_few<XG, NT, WAVES, false>), grid, block, 0, st, a);
   return hipGetLastError();
+}
+// Tiles of 16 to 64 outputs: those that give the busiest compute unit the fewest, and
+// of these the widest, which read the tokens the least often.  16 x 22016 x 4096: 20.1 us
+// with 48, 20.8 with 32, 21.0 with 64; 16 x 11008 x 4096: 11.8 with 48, 14.2 with 16;
+// 16 x 16384 x 4096: 16.4 with 64, 17.8 with 32; 1 x 4096 x 4096: 5.9 with 16, 7.3 with 32.
+template <int XG>
+hipError_t few_rows(const Int8Args& a, hipStream_t st) {
+  int wide = 1, least = 1 << 30;
+  for (int nt = 1; nt <= 4; ++nt) {
+    const int most = ((a.N + 16 * nt - 1) / (16 * nt) + 255) / 256 * nt;
+    if (most <= least) {
+      least = most;
+      wide = nt;
+    }
+  }
+  switch (wide) {
+    case 1: return few<XG, 1, 8>(a, st);
+    case 2: return few<XG, 2, 4>(a, st);
+    case 3: return few<XG, 3, 4>(a, st);
+    default: return few<XG, 4, 4>(a, st);
+  }
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES>
@@ -574,9 +597,9 @@ size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 }
 
 hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
-  if (a.M <= 8) return few<1, 1, 8>(a, 512, st);
-  if (a.M <= 16) return a.N < 16384 ? few<2, 1, 8>(a, 256, st) : few<2, 2, 4>(a, 512, st);
-  if (few_tokens(a.M, a.N)) return few<4, 1, 8>(a, 256, st);
+  if (a.M <= 8) return few_rows<1>(a, st);
+  if (a.M <= 16) return few_rows<2>(a, st);
+  if (few_tokens(a.M, a.N)) return few<4, 1, 8>(a, st);
   const Choice c = choose(a.M, a.N, a.K, a.ws != nullptr);
   hipError_t e;
   switch (c.form) {

@@ -85,12 +85,8 @@ def test_the_largest_sums_are_exact(M):
         assert (y.cpu().numpy() == np.float32(total)).all() and abs(total) < 2 ** 31
 
 
-@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 384, 400, 528, 1296])
-@pytest.mark.parametrize("M,N", [(1025, 18003), (700, 30005), (3900, 4090), (255, 33000), (2040, 4005)])
-def test_the_largest_tiles(M, N, K):
-    """256 tokens by 128 to 384 outputs a workgroup, with rows, outputs and depths that end inside a tile.  The sums
-    are exact in fp64 too, and each later step is one fp32 operation."""
-    torch = torch_cuda()
+def check_on_gpu(torch, M, N, K):
+    """The sums are exact in fp64 too, and each later step is one fp32 operation."""
     import paper_2406_13868_amd as sdq
     dt = [torch.bfloat16, torch.float32][K // 16 % 2]
     say(M, N, K, dt)
@@ -100,6 +96,21 @@ def test_the_largest_tiles(M, N, K):
     if bias is not None:
         want = want + bias
     assert torch.equal(y, want.to(dt))
+
+
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 384, 400, 528, 1296])
+@pytest.mark.parametrize("M,N", [(1025, 18003), (700, 30005), (3900, 4090), (255, 33000), (2040, 4005)])
+def test_the_largest_tiles(M, N, K):
+    """256 tokens by 128 to 384 outputs a workgroup, with rows, outputs and depths that end inside a tile."""
+    check_on_gpu(torch_cuda(), M, N, K)
+
+
+@pytest.mark.parametrize("K", [16, 144, 640, 1040, 1168])
+@pytest.mark.parametrize("N", [4096, 4097, 5003, 8192, 11001, 12288, 12289, 16370, 22013, 33001])
+def test_few_tokens_by_many_outputs(N, K):
+    """Tiles of 16 to 64 outputs, one or several a workgroup, the last one short."""
+    for M in (1, 8, 9, 16, 30):
+        check_on_gpu(torch_cuda(), M, N, K)
 
 
 DIVIDED = [(64, 4096, 16384), (100, 300, 8208), (40, 37, 13456), (130, 1000, 8192), (33, 4, 4096), (600, 601, 6000)]
