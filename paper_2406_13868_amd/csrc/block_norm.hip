@@ -135,18 +135,22 @@ struct Weights {
         for (int c = 0; c < CH; ++c) b[c].load(br, t + c * nt);
       }
   }
-  // v = d * rstd * w + b, d = v - mean
-  __device__ __forceinline__ void apply(float (&v)[CH][8], double mean, float rstd, bool bias) const {
+  // v = d * rstd * w + b, d = v - mean.  Places past the row's P pieces stay 0, whatever
+  // the mean and the root are: they take part in the maximum and the sums that follow.
+  __device__ __forceinline__ void apply(float (&v)[CH][8], uint32_t t, int nt, uint32_t P, double mean, float rstd, bool bias) const {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      const bool inside = t + c * nt < P;
+      const float by = inside ? rstd : 0.f;
       float g[8];
       w[c].widen(g);
       if constexpr (LAYER) {
+        const double mu = inside ? mean : 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mean);
+        for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mu);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * g[i];
+      for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * by * g[i];
       if constexpr (LAYER)
         if (bias) {
           b[c].widen(g);
@@ -209,7 +213,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArg
         double mean;
         float rstd;
         stats<LAYER, NT, CH>(u, t, P, a.per, a.post_eps, red[turn], mean, rstd);
-        pw.apply(u, mean, rstd, a.post_bias != nullptr);
+        pw.apply(u, t, NT, P, mean, rstd, a.post_bias != nullptr);
       }
       if (cols) {
 #pragma unroll
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void block_norm_kernel(NormArg
       double mean;
       float rstd;
       stats<LAYER, NT, CH>(r, t, P, a.per, a.eps, red[turn] + 2 * (NT / 64), mean, rstd);
-      w.apply(r, mean, rstd, a.bias != nullptr);
+      w.apply(r, t, NT, P, mean, rstd, a.bias != nullptr);
       const int64_t to = int64_t(m) * K;
       if (a.out_type == kF32) {
 #pragma unroll
