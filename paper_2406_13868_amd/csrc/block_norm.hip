@@ -77,6 +77,14 @@ __device__ __forceinline__ void apply(float (&v)[8], bool layer, double mean, fl
   }
 }
 
+// sum / K with the rounding of a division: the product by the rounded 1 / K, and the
+// rest that it leaves times 1 / K.  (The product alone is a step off for some K: the
+// mean of K = 392 ones was not 1, and what it left of the row was normed.)
+__device__ __forceinline__ double mean_of(double sum, double K, double per) {
+  const double q = sum * per;
+  return __builtin_fma(__builtin_fma(-q, K, sum), per, q);
+}
+
 // 1 / sqrt(sum / K + eps): the reciprocal root instruction is 2^-24 off or better,
 // two steps of Newton's leave fp64's own roundings.  (The division and the root that
 // the compiler makes are 150 instructions for every thread.)
@@ -87,7 +95,6 @@ __device__ __forceinline__ float root(double sum, double per, double eps) {
   for (int i = 0; i < 2; ++i) y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
   return x == __builtin_huge_val() ? 0.f : float(y);
 }
-
 
 // Mean (layer only) and reciprocal root of a held row, whose places past its end are 0.
 template <bool LAYER, int NT, int CH>
@@ -100,7 +107,7 @@ __device__ __forceinline__ void stats(const float (&v)[CH][8], uint32_t t, uint3
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += double(v[c][i]);
-    mean = row_sum<NT>(s, red) * per;
+    mean = mean_of(row_sum<NT>(s, red), 8.0 * P, per);
     s = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -311,7 +318,7 @@ __global__ __launch_bounds__(1024) void block_norm_wide(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += double(v[i]);
       }
-      mu = row_sum<NT>(s, red0) * a.per;
+      mu = mean_of(row_sum<NT>(s, red0), double(a.K), a.per);
     }
     double s = 0.0;
     for (int64_t k = threadIdx.x * 8; k < K; k += NT * 8) {

@@ -49,3 +49,21 @@ def test_large_constant_rows(K, top):
         # the block's output normed before it joins the stream
         got = sdq.block_norm(res, x, W, B, layer=True, post_weight=PW, post_bias=PB, scale=0.5, out_dtype=out)
         check(torch, got, None, O.stream_steps(other, rows, None, 0.5, pw, pb, 1e-6, True), w, b, 1e-6, out)
+
+
+# Widths whose reciprocal in 64 bits times the width is not 1, in every form of the kernel, and some where it is.
+@pytest.mark.parametrize("K", [64, 392, 784, 1288, 1568, 2576, 4488, 8976, 17720, 40960])
+@pytest.mark.parametrize("eps", [1e-6, 1e-30])
+def test_the_mean_of_a_constant_row_is_that_constant(K, eps):
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    rows = np.repeat(np.array([1.0, -3.3, 0.1, 7e-5, 1e3, 123456.7], np.float32)[:, None], K, 1)
+    w = np.ones(K, np.float32)
+    x, W = torch.from_numpy(rows).cuda(), torch.from_numpy(w).cuda()
+    for out in OUTS:
+        say(K, eps, out)
+        _, n, s = got = sdq.block_norm(x, weight=W, layer=True, eps=eps, out_dtype=out)
+        assert (n == 0).all() and (s is None or (s == 0).all())
+        check(torch, got, rows, None, w, None, eps, out)
+        got = sdq.block_norm(torch.zeros_like(x), x, W, layer=True, post_weight=W, eps=eps, out_dtype=out)
+        check(torch, got, None, O.stream_steps(np.zeros_like(rows), rows, None, 1.0, w, None, eps, True), w, None, eps, out)
