@@ -243,6 +243,17 @@ def glu_act(x, act: str = "silu", gated: bool = True, out_dtype=None, out=None, 
     return out, scales
 
 
+def _product_type(out_dtype):
+    """The torch dtype of a product's output, given as such or by its name."""
+    try:
+        want, code = _OUT[out_dtype]
+    except (KeyError, TypeError):
+        code = _CODES
+    if code >= _CODES:
+        raise ValueError("out_dtype must be float32 or bfloat16, as 'f32', 'bf16' or a torch dtype")
+    return want
+
+
 @functools.lru_cache(maxsize=4096)
 def gemm_int8_workspace_size(M: int, N: int, K: int) -> int:
     """Device workspace bytes that gemm_int8 takes for these sizes (0: none)."""
@@ -258,7 +269,7 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
     block_norm and glu_act write (rows may be strided); s_x fp32 [M], s_w fp32 [N],
     bias fp32 [N].  The codes and scales of a weight are quantize_act(W, cfg) with
     int8 activations, once.  out: [M, N], fp32 or bf16, rows may be strided; or
-    out_dtype (default fp32).  workspace: a uint8 tensor of gemm_int8_workspace_size
+    out_dtype, 'f32' (the default), 'bf16' or a torch dtype.  workspace: a uint8 tensor of gemm_int8_workspace_size
     bytes, or a fresh one is made where that is not 0."""
     _, M, K, x_ld, x_at, index = _first(xq, "xq")
     _, N, depth, w_ld, w_at, where = _first(wq, "wq")
@@ -270,10 +281,12 @@ def gemm_int8(xq, s_x, wq, s_w, bias=None, out=None, out_dtype=None, workspace=N
     dt = wq.dtype
     if dt is not _i8 and dt is not _u8:
         _wrong(wq, "wq", kinds="int8 codes (int8 or uint8)")
+    if out_dtype is not None:
+        out_dtype = _product_type(out_dtype)
     if out is None:
-        out = _empty((M, N), _f32 if out_dtype is None else out_dtype, xq.device, stream)
-    elif out_dtype is not None and out.dtype is not out_dtype:
-        raise ValueError(f"out must be {out_dtype}")
+        out = _empty((M, N), out_dtype or _f32, xq.device, stream)
+    elif out_dtype is not None and getattr(out, "dtype", None) is not out_dtype:
+        raise ValueError(f"out must be a tensor of {out_dtype}")
     y_ld, y_at = _like(out, (M, N), "out", index)
     need = gemm_int8_workspace_size(M, N, K)
     ws = ws_bytes = 0

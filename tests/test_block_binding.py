@@ -138,3 +138,12 @@ def test_outputs_that_are_no_tensors():
     for out_dtype in (None, "int8", "bf16"):
         scales = torch.zeros(3) if out_dtype == "int8" else None
         _raises(lambda: block._result([1.0], scales, out_dtype, (3, 16), (3,), like, -1, None), "out must be a torch tensor")
+
+
+def test_the_types_of_a_products_output():
+    block._prepare()
+    for dt in (torch.float32, torch.bfloat16):
+        assert block._product_type(dt) is dt
+    assert block._product_type("f32") is torch.float32 and block._product_type("bf16") is torch.bfloat16
+    for out_dtype in ("int8", "e4m3", "f16", torch.float16, 3, [torch.float32]):
+        _raises(lambda: block._product_type(out_dtype), "float32 or bfloat16")

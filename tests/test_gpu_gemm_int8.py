@@ -203,3 +203,20 @@ def test_calls_without_rows_and_calls_that_are_refused():
     refused("SHAPE", x[:, :40], s3, w[:, :40], s5)
     refused("SHAPE", x[:, 1:49], s3, w[:, :48], s5)
     refused("contiguous", x.t().contiguous().t(), s3, w, s5)
+
+
+def test_the_names_of_output_types_and_outputs_that_are_no_tensors():
+    torch = torch_cuda()
+    import paper_2406_13868_amd as sdq
+    (x, sx, w, sw), bias, _, _ = make(torch, 1, 5, 40, 64)
+    for name, dt in (("f32", torch.float32), ("bf16", torch.bfloat16)):
+        y = sdq.gemm_int8(x, sx, w, sw, bias=bias, out_dtype=name)
+        assert y.dtype is dt and torch.equal(y, sdq.gemm_int8(x, sx, w, sw, bias=bias, out_dtype=dt))
+        assert sdq.gemm_int8(x, sx, w, sw, out=y, out_dtype=name) is y
+    for out_dtype in ("int8", "e4m3", "f16", torch.float16, 3, [torch.float32]):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            sdq.gemm_int8(x, sx, w, sw, out_dtype=out_dtype)
+    for out in ([1.0], x.cpu().numpy(), torch.empty((5, 40), dtype=torch.float64, device="cuda")):
+        for out_dtype in (None, "bf16", torch.float32):
+            with pytest.raises(ValueError, match="out must be"):
+                sdq.gemm_int8(x, sx, w, sw, out=out, out_dtype=out_dtype)
