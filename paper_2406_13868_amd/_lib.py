@@ -197,6 +197,15 @@ def kernel_name(cfg: "sdq_config", M: int, N: int, K: int, path: int = PATH_AUTO
     return out.value.decode()
 
 
+def int8_kernel_name(M: int, N: int, K: int, workspace: bool = True) -> str:
+    """The form that gemm_int8 takes for these sizes, by the launcher's own rules: for tests."""
+    out = C.create_string_buffer(64)
+    fn = lib().sdq_gemm_int8_kernel_name
+    fn.restype, fn.argtypes = C.c_int, [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_char_p, C.c_size_t]
+    check(fn(M, N, K, workspace, out, len(out)), "sdq_gemm_int8_kernel_name")
+    return out.value.decode()
+
+
 def check(status: int, what: str) -> None:
     if status != SDQ_OK:
         raise SDQError(status, what)

@@ -136,6 +136,14 @@ extern "C" sdq_status sdq_gemm_int8_workspace_size(int64_t M, int64_t N, int64_t
   return SDQ_OK;
 }
 
+// Not part of the C ABI (no declaration in sdq.h): the form of a product for the tests.
+extern "C" sdq_status sdq_gemm_int8_kernel_name(int64_t M, int64_t N, int64_t K, int32_t divide, char* out, size_t bytes) {
+  if (!out) return SDQ_ERR_NULL;
+  if (M < 1 || !int8_fits(M, N, K)) return SDQ_ERR_SHAPE;
+  gemm_int8_kernel_name(M, N, K, divide != 0, out, bytes);
+  return SDQ_OK;
+}
+
 extern "C" sdq_status sdq_gemm_int8(const sdq_int8_args* t, void* stream) {
   if (!t) return SDQ_ERR_NULL;
   if (!activations(t->y_dtype)) return SDQ_ERR_CONFIG;

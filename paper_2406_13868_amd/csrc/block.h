@@ -46,6 +46,8 @@ struct Int8Args {
   void* ws;  // gemm_int8_workspace_bytes bytes, or NULL: K is not divided
 };
 size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+// The form that a product takes, with or without a workspace, for the tests.
+void gemm_int8_kernel_name(int64_t M, int64_t N, int64_t K, bool divide, char* out, size_t n);
 hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st);
 
 }  // namespace sdq

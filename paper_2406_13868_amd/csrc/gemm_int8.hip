@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <cstdio>
 
 #include "block.h"
 #include "kernels.h"
@@ -490,17 +491,21 @@ hipError_t few(const Int8Args& a, hipStream_t st) {
 // of these the widest, which read the tokens the least often.  16 x 22016 x 4096: 20.1 us
 // with 48, 20.8 with 32, 21.0 with 64; 16 x 11008 x 4096: 11.8 with 48, 14.2 with 16;
 // 16 x 16384 x 4096: 16.4 with 64, 17.8 with 32; 1 x 4096 x 4096: 5.9 with 16, 7.3 with 32.
-template <int XG>
-hipError_t few_rows(const Int8Args& a, hipStream_t st) {
-  int wide = 1, least = 1 << 30;
+int few_width(int64_t N) {
+  int wide = 1;
+  int64_t least = int64_t(1) << 30;
   for (int nt = 1; nt <= 4; ++nt) {
-    const int most = ((a.N + 16 * nt - 1) / (16 * nt) + 255) / 256 * nt;
+    const int64_t most = ((N + 16 * nt - 1) / (16 * nt) + 255) / 256 * nt;
     if (most <= least) {
       least = most;
       wide = nt;
     }
   }
-  switch (wide) {
+  return wide;
+}
+template <int XG>
+hipError_t few_rows(const Int8Args& a, hipStream_t st) {
+  switch (few_width(a.N)) {
     case 1: return few<XG, 1, 8>(a, st);
     case 2: return few<XG, 2, 4>(a, st);
     case 3: return few<XG, 3, 4>(a, st);
@@ -594,6 +599,16 @@ size_t gemm_int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   if (few_tokens(M, N)) return 0;
   const int parts = choose(M, N, K, true).parts;
   return parts == 1 ? 0 : size_t(M) * size_t(N) * size_t(parts) * 4;
+}
+
+void gemm_int8_kernel_name(int64_t M, int64_t N, int64_t K, bool divide, char* out, size_t n) {
+  if (few_tokens(M, N)) {
+    std::snprintf(out, n, "few %dx%d", M <= 8 ? 8 : M <= 16 ? 16 : 32, M <= 16 ? 16 * few_width(N) : 16);
+    return;
+  }
+  const Choice c = choose(M, N, K, divide);
+  const Form& f = kForms[c.form];
+  std::snprintf(out, n, "tile %dx%d%s (%d part%s)", f.bm, f.bn, f.two > 0 ? " in pairs" : "", c.parts, c.parts == 1 ? "" : "s");
 }
 
 hipError_t launch_gemm_int8(const Int8Args& a, hipStream_t st) {
