@@ -142,19 +142,18 @@ struct Weights {
         for (int c = 0; c < CH; ++c) b[c].load(br, t + c * nt);
       }
   }
-  // v = d * rstd * w + b, d = v - mean.  Places past the row's P pieces stay 0, whatever
-  // the mean and the root are: they take part in the maximum and the sums that follow.
+  // v = d * rstd * w + b, d = v - mean.  Places past the row's P pieces, which take part in
+  // the maximum and the sums that follow, become 0 with any mean of finite numbers, which is
+  // a finite fp32 too; with any other the whole row is NaN.
   __device__ __forceinline__ void apply(float (&v)[CH][8], uint32_t t, int nt, uint32_t P, double mean, float rstd, bool bias) const {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const bool inside = t + c * nt < P;
-      const float by = inside ? rstd : 0.f;
+      const float by = t + c * nt < P ? rstd : 0.f;
       float g[8];
       w[c].widen(g);
       if constexpr (LAYER) {
-        const double mu = inside ? mean : 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mu);
+        for (int i = 0; i < 8; ++i) v[c][i] = float(double(v[c][i]) - mean);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * by * g[i];
