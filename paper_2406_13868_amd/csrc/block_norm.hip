@@ -13,9 +13,11 @@
 //
 // A row is held in registers by a wave or a workgroup, in pieces of eight
 // elements, and read and written once: 8192 x 4096, bf16 with post-norm, gates and int8
-// codes, takes 47.7 us, 4.9 TB/s, the rate of a large copy; a single row 2.8 us, the
-// latency of a load and of each sum.  Rows of more than kMostHeld elements are
-// read again for each sum instead.
+// codes, takes 47.6 us among other calls, 4.9 TB/s, the rate of a large copy (51 to 53
+// captured and back to back); a single row 2.8 us, the latency of a load and of each
+// sum.  Rows of more than kMostHeld elements are read again for each sum instead
+// (1024 x 24576, bf16, post-norm, gates, int8 codes: 87 us, layer norm 125; a copy's
+// rate would be 35).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -370,7 +372,9 @@ void launch_rows(const NormArgs& a, hipStream_t st) {
 template <bool XF32, int YT, int NT, int CH>
 void launch(const NormArgs& a, hipStream_t st) {
   // 1024 threads have 128 registers each: a layer norm's weights and biases, or an fp32
-  // block's rows, would leave them (1024 x 16384, fp32: 68 us; 60 with 512 threads).
+  // block's rows, would leave them (rms, 1024 x 16384, fp32: 68 us; 60 with 512 threads).
+  // A layer norm's do not fit the 256 of 512 threads either: it spills 10 (bf16 both) to
+  // 103 (fp32 both) and takes 88 and 145 us for 2048 x 16384, at a copy's rate 47 and 87.
   constexpr bool kMost = NT == 1024;
   if (a.layer) launch_rows<XF32, YT, true, kMost ? 512 : NT, kMost ? 2 * CH : CH>(a, st);
   else launch_rows<XF32, YT, false, kMost && YT == kF32 ? 512 : NT, kMost && YT == kF32 ? 2 * CH : CH>(a, st);
@@ -393,10 +397,12 @@ void launch(const NormArgs& a, hipStream_t st) {
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t st) {
   // The fewest registers a thread that hold a row, so that few rows end soonest; of many
   // rows two pieces a thread, where half as many threads meet for a row's sums.  Measured
-  // (bf16, post-norm, gates, int8 codes; the form taken, then the other):
-  //   64 x 1024: 3.1 us (128 threads of one piece), 3.3;  8192 x 1024: 14.9, 16.4
-  //   64 x 4096: 3.7 (512 of one), 3.9;  512 x 4096: 6.1, 6.1;  8192 x 4096: 52.7, 55.5
-  //   64 x 8192: 4.7 (512 of two), 5.0 (1024 of one);  4096 x 8192: 53.2, 61.2
+  // captured and back to back (us; bf16, rms, post-norm, gates, int8 codes):
+  //   1024 wide, one piece a thread and two: 64 rows 3.1, 3.3;  512 rows 3.7, 3.5;  8192 rows 15.9, 14.5
+  //   2048: 64 rows 3.3, 3.6;  512 rows 4.1, 4.6;  1024 rows 6.1, 5.9;  8192 rows 30.5, 28.3
+  //   4096: 64 rows 3.7, 3.8;  512 rows 6.2, 6.2;  1024 rows 10.5, 9.6;  8192 rows 56.4, 51.5
+  // and wider rows, the form taken and the other:
+  //   64 x 8192: 4.7 (512 threads of two pieces), 5.0 (1024 of one);  4096 x 8192: 53.2, 61.2
   //   64 x 16384: 6.6 (1024 of two), 6.5 (512 of four);  2048 x 16384: 57.4, 67.3
   const uint32_t P = a.K / 8;
   const bool many = a.M >= 512;

@@ -30,7 +30,8 @@ constexpr int kStream = 2;
 // awaited by the kernels themselves: a read of shared memory waits for every request
 // that the compiler knows of and cannot tell from it, and it loses count where a loop
 // closes (256 x 4096 x 4096: 13.0 us that way, 10.5 this).  The instruction returns
-// nothing to registers; nothing else here uses m0.
+// nothing to registers.  m0 is a register that the compiler keeps no value in (it takes
+// no clobber of it), and it writes it for no other instruction of these kernels.
 template <int HINT = 0>
 __device__ __forceinline__ void request_1k(__amdgpu_buffer_rsrc_t from, uint8_t* to, uint32_t at, uint32_t base) {
   const uint32_t where = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)to));
@@ -69,12 +70,12 @@ constexpr int kSums = 4;  // beside kF32 and kBF16: int32 sums, not scaled yet
 // (their results are not stored), and the pieces of 16 past the end of K are the last
 // piece again, with zeros in their place on the tokens' side.
 //
-// What bounds a large product is the way of the tiles' bytes to the compute units, which
-// takes 18 bytes a clock each from the L2s with a quarter of the lines missing there: the
-// requests alone are 327 us of 4096 x 22016 x 4096 in tiles of 256 x 256, the matrix
-// instructions alone 220 to 250 (the clock falls under them).  256 x 384 is the largest
-// tile whose sums, operands and two chunks fit: it asks for a sixth less, and the whole
-// is 332 us, 2.2 POP/s (256 x 256: 369; the library's product of the codes: 339 to 355).
+// What bounds a large product is how far its requests and its matrix instructions run
+// beside each other: of 4096 x 22016 x 4096 the requests alone are 262 us (327 in tiles of
+// 256 x 256), the matrix instructions alone 220 to 250, at the clock that random codes
+// leave them.  256 x 384 is the largest tile whose sums, operands and two chunks fit: it
+// asks for a sixth less, and the whole is 328 to 332 us, 2.2 POP/s (256 x 256: 369; the
+// library's product of the codes: 339 to 355).
 // Deeper stages of half chunks, and four waves of 128 x 128: no faster.
 //
 // In a stage, row r's piece p (16 bytes) lies at r * 128 + 16 * (p ^ (r / 2 & 7)):
@@ -307,8 +308,8 @@ __global__ __launch_bounds__(256) void gemm_int8_join(Int8Args a, const int32_t*
 // by integer atomics.  Whole lines of rows are requested, in the order that spreads
 // them over the banks.  (In the operands' own order, straight to registers, lanes
 // that follow each other take four rows, which costs the address units three times as
-// much: 2.9 TB/s with 16 tokens.)  16 x 22016 x 4096: 17.8 us, 5.1 TB/s; 1 x 4096 x
-// 4096: 5.8, of which 3 are the bytes.
+// much: 2.9 TB/s with 16 tokens.)  16 x 22016 x 4096: 17.8 us among other calls, 5.1
+// TB/s; 1 x 4096 x 4096: 5.8, of which 3 are the bytes.
 //
 // 16x16x64: A = 16 rows of W, B = 16 tokens, 16 bytes of K a lane (lane l: row or
 // token l & 15, bytes 16 (l >> 4)); the sums leave a lane four outputs of a token.
@@ -488,7 +489,8 @@ hipError_t few(const Int8Args& a, hipStream_t st) {
   return hipGetLastError();
 }
 // Tiles of 16 to 64 outputs: those that give the busiest compute unit the fewest, and
-// of these the widest, which read the tokens the least often.  16 x 22016 x 4096: 20.1 us
+// of these the widest, which read the tokens the least often.  Captured and back to back
+// (the first of these 2.5 us more than among other calls): 16 x 22016 x 4096: 20.1 us
 // with 48, 20.8 with 32, 21.0 with 64; 16 x 11008 x 4096: 11.8 with 48, 14.2 with 16;
 // 16 x 16384 x 4096: 16.4 with 64, 17.8 with 32; 1 x 4096 x 4096: 5.9 with 16, 7.3 with 32.
 int few_width(int64_t N) {
@@ -543,7 +545,9 @@ hipError_t join(const Int8Args& a, int parts, hipStream_t st) {
 // units, or twice as many workgroups where two fit, `one` (`two`) a chunk of K and 2
 // for its beginning and end.  Measured at 256 to 4096 tokens by 4096 outputs (the wide
 // forms: 256 to 16384 by 4096 to 22016), K = 4096 and, where rows are not whole cache
-// lines and a chunk of each takes two, 4112.  The form taken and the nearest other, at
+// lines and a chunk of each takes two, 4112.  It counts no weights' bytes from memory: where those
+// bound a call, as of 17 to 64 tokens by many outputs, the forms are ranked by their
+// chunks alone.  The form taken and the nearest other, calls from Python in a row, at
 // K = 4096: 256 x 22016: 35.5 us (256 x 128), 46.3 (two of 128 x 128); 512 x 22016: 56.6
 // (256 x 192), 61.9 (128 x 384, dropped); 4096 x 4096: 67 (256 x 256), 77 (256 x 128);
 // 2048 x 11008: 84 (256 x 384), 106 (256 x 256); 1024 x 4096: 26 (128 x 128), 32
@@ -589,8 +593,10 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool divide) {
   return best;
 }
 
-// Measured: 20 x 512 x 4096: 4.9 us, 8.6 by tiles; 32 x 4096 x 4096: 7.7 and 10;
-// 32 x 8192 x 4096: 13.4 and 10.5.
+// Up to 4096 outputs each of 256 compute units has one tile of 16 at most.  Measured
+// captured and back to back, K = 4096, this form and tiles: 20 x 512: 6.5 us, 7.3;
+// 17 x 4096: 7.2, 9.0;  32 x 4096: 7.8, 10.0;  17 x 5120: 10.3, 9.6;  32 x 5120: 11.4, 9.4;
+// 32 x 8192: 12.7, 9.8.
 bool few_tokens(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N <= 4096); }
 
 }  // namespace

@@ -8,7 +8,8 @@
 // is evaluated in fp64 and rounded to fp32 once: two evaluations of exp that
 // differ in an fp32's last bit would give other codes now and then.  That makes the
 // vector units the bound, 39 instructions an element, two thirds of them fp64:
-// 4096 x 11008, gated silu to int8 codes, takes 58 us (82% busy), its bytes alone 45.
+// 4096 x 11008, gated silu to int8 codes, takes 58 us among other calls (82% busy; 64 to 69
+// back to back, where the clock falls), its bytes alone 45.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -23,10 +24,11 @@ namespace {
 
 constexpr uint32_t kMostHeld = 32768;
 
-// exp(t) within 2e-14 of itself for |t| <= 700: t = n ln 2 + r with |r| <= ln 2 / 2,
+// exp(t) within 4.3e-14 of itself for |t| <= 700: t = n ln 2 + r with |r| <= ln 2 / 2,
 // exp(r) by the polynomial of degree 9 that meets it at the ten Chebyshev nodes of
 // that range (1.9e-14 off at most), times 2^n, whose n is the low word of
-// t / ln 2 + 1.5 * 2^52.
+// t / ln 2 + 1.5 * 2^52.  (n ln 2 is off by n times the 2.3e-17 that ln 2 loses in one
+// word: 2.3e-14 where |n| is 1010, and 3e-15 up to |t| = 88, where fp32's range ends.)
 __device__ __forceinline__ double exp64(double t) {
   const double shifted = __builtin_fma(t, 1.4426950408889634, 0x1.8p52);
   const double r = __builtin_fma(shifted - 0x1.8p52, -0.6931471805599453, t);
@@ -189,12 +191,14 @@ template <int ACT, bool XF32, bool GATED>
 void launch(const GluArgs& a, hipStream_t st) {
   // Few rows end soonest on many threads, as long as no wave waits for many others; many
   // rows keep the fp64 units busiest with few threads, of which some workgroups load
-  // while others compute.  Measured (bf16, gated silu, int8 codes; the form taken, then
-  // the other):
-  //   64 x 2048: 3.1 us (256 threads of one piece), 4.8;  8192 x 2048: 24.6 (64 of four), 35.1
-  //   1 x 4096: 3.1 (256 of two), 3.4 (512 of one);  8192 x 4096: 46.4, 74.9
-  //   1 x 8192: 4.0 (512 of two), 4.6 (256 of four);  4096 x 8192: 48.1 (256 of four), 74.8 (1024 of one)
-  //   1 x 11008: 4.7 (1024 of two), 6.3;  4096 x 11008: 63.0 (256 of eight), 81.6
+  // while others compute.  Measured captured and back to back (us; bf16, gated silu, int8
+  // codes), the form for few rows and the one for many:
+  //   1024 wide: 64 rows 2.9, 3.2;  512 rows 4.0, 3.4;  4096 rows 10.5, 8.1
+  //   2048: 64 rows 2.9, 4.7;  512 rows 4.1, 5.0;  1024 rows 6.1, 5.3;  4096 rows 17.9, 13.7
+  //   8192: 64 rows 4.3, 4.9;  512 rows 8.0, 9.0;  1024 rows 12.8, 13.8;  4096 rows 47.4, 47.3
+  //   11008: 64 rows 5.0, 6.7;  512 rows 11.6, 12.0;  1024 rows 20.4, 18.2;  4096 rows 77.7, 64.4
+  // and 1 x 4096: 3.1 (256 threads of two pieces), 3.4 (512 of one);  8192 x 4096: 46.4, 74.9.
+  // Rows past kMostHeld are evaluated twice (1024 x 40960: 111 us, at a copy's rate 42).
   const uint32_t P = a.F / 8;
   const bool many = a.M >= 512;
   if (a.out_type == kF32 || a.out_type == kBF16) {
